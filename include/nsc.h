@@ -448,6 +448,104 @@ int nsc_threshold_sweep(const nsc_sweep_cfg* cfg, const double* score, const flo
                         const uint8_t* truth, int64_t n, const double* deltas, int32_t n_t,
                         nsc_sweep_row* rows, int32_t* best, void* stream);
 
+/* ------------------------------------------------------------------------
+ * Single layers of a network on the caller's own tensors: what a program
+ * needs that builds or fits networks beside the cascade.  Tensors are device
+ * memory of one element type (NSC_T_*), aligned to that type; statistics,
+ * sums and the parameters marked float are fp32.  `count` (device, one int32,
+ * nullable) holds the number of images or rows there are, of at most
+ * max_count (NULL: max_count); what lies behind them is neither read nor
+ * written.  An image's or row's result does not depend on the others of a call
+ * (max_count may decide in which order its fp32 sums are taken).
+ * Each call needs its own workspace until its work has run; workspaces are
+ * 256-byte aligned, and no call allocates or records anything but kernels. */
+enum { NSC_T_F32 = 0, NSC_T_BF16 = 1, NSC_T_F16 = 2 };
+enum { NSC_ACT_NONE = 0, NSC_ACT_RELU = 1, NSC_ACT_SILU = 2 };
+/* Most channels of a map, and most channels of one of its groups. */
+enum { NSC_MAX_NORM_CHANNELS = 65536, NSC_MAX_NORM_GROUP = 1024 };
+
+/* Group normalisation of channels-last maps with an activation.  Image i is
+ * [h][w][c] at element i * x_stride (y_stride) of x and dx (y and dy). */
+typedef struct nsc_norm_desc {
+  int32_t h, w, c;
+  int32_t groups;             /* divides c; group g is channels g c / groups ..  */
+  int32_t act;                /* NSC_ACT_*                                       */
+  int32_t dtype;              /* NSC_T_* of x, y, dy and dx                      */
+  float eps;                  /* added to the variance; finite, > 0              */
+  int64_t x_stride, y_stride; /* elements between images, >= h * w * c           */
+} nsc_norm_desc;
+
+/* Validates a description without touching the GPU. */
+int nsc_norm_check(const nsc_norm_desc* desc);
+/* Workspace of nsc_group_norm (backward = 0) or nsc_group_norm_backward
+ * (backward = 1) for up to max_count images. */
+int nsc_group_norm_workspace_bytes(const nsc_norm_desc* desc, int64_t max_count, int32_t backward,
+                                   size_t* bytes);
+/* For every image and group, over its h * w * c / groups values x:
+ *   mean, var = mean of (x - mean)^2, rstd = 1 / sqrt(var + eps),
+ *   y = act(gamma[ch] * (x - mean) * rstd + beta[ch]), rounded once.
+ * gamma, beta (device, c floats); stats (device, nullable): (mean, rstd) of
+ * image i and group g at 2 * (i * groups + g).  y may be x itself when the
+ * strides are equal.  Errors: NSC_E_INVAL, NSC_E_SHAPE, NSC_E_DTYPE,
+ * NSC_E_WORKSPACE, NSC_E_HIP. */
+int nsc_group_norm(const nsc_norm_desc* desc, const void* x, const float* gamma, const float* beta,
+                   const int32_t* count, int64_t max_count, void* y, float* stats, void* ws,
+                   size_t ws_bytes, void* stream);
+/* The gradients of the above for the gradient dy of its output, from the same
+ * x and the stats it wrote.  With xh = (x - mean) * rstd, z = gamma xh + beta
+ * and dz = dy * act'(z) (ReLU: dy where z > 0, decided exactly):
+ *   dbeta[ch] = sum dz, dgamma[ch] = sum dz xh over all images and pixels,
+ *   dx = rstd (gamma dz - m1 - xh m2), m1 and m2 the means of gamma dz and of
+ *   gamma dz xh over the image's group.
+ * dx as x; dgamma, dbeta (device, c floats) are written, zeros without
+ * images.  The sums are taken in a fixed order.  Errors as above. */
+int nsc_group_norm_backward(const nsc_norm_desc* desc, const void* x, const void* dy,
+                            const float* gamma, const float* beta, const float* stats,
+                            const int32_t* count, int64_t max_count, void* dx, float* dgamma,
+                            float* dbeta, void* ws, size_t ws_bytes, void* stream);
+
+/* A projection that all rows share, each row with the low-rank adapter of its
+ * camera (or request) beside it.  Row r is k values at element r * x_stride of
+ * x and dx, and d values at r * y_stride of y and dy. */
+enum { NSC_MAX_RANK = 128, NSC_MAX_ADAPTERS = 65535 };
+typedef struct nsc_adapter_desc {
+  int32_t k, d;               /* inputs and outputs of the projection            */
+  int32_t rank;               /* of every adapter, 1 .. NSC_MAX_RANK             */
+  int32_t n_adapters;         /* 1 .. NSC_MAX_ADAPTERS                           */
+  int32_t dtype;              /* NSC_T_* of x, w, a, b, y, dy and dx             */
+  int64_t x_stride, y_stride; /* elements between rows, >= k and >= d            */
+} nsc_adapter_desc;
+
+/* Validates a description without touching the GPU. */
+int nsc_adapter_check(const nsc_adapter_desc* desc);
+/* Workspace of nsc_adapter_project (backward = 0) or nsc_adapter_backward
+ * (backward = 1) for up to max_rows rows. */
+int nsc_adapter_workspace_bytes(const nsc_adapter_desc* desc, int64_t max_rows, int32_t backward,
+                                size_t* bytes);
+/* With p = ids[r] the adapter of row r,
+ *   y[r] = x[r] w^T + bias + scale[p] (x[r] a[p]^T) b[p]^T, rounded once.
+ * w (device, [d][k]); bias (device, d floats, nullable); a (device,
+ * [n_adapters][rank][k]); b (device, [n_adapters][d][rank]); scale (device,
+ * n_adapters floats); ids (device, int32 per row, in any order): a row whose
+ * id lies outside 0 .. n_adapters - 1 (such as -1) has no adapter.  y must not
+ * overlap the inputs.  Errors: NSC_E_INVAL, NSC_E_SHAPE, NSC_E_DTYPE,
+ * NSC_E_WORKSPACE, NSC_E_HIP. */
+int nsc_adapter_project(const nsc_adapter_desc* desc, const void* x, const void* w,
+                        const float* bias, const void* a, const void* b, const float* scale,
+                        const int32_t* ids, const int32_t* count, int64_t max_rows, void* y,
+                        void* ws, size_t ws_bytes, void* stream);
+/* The gradients of the above for the gradient dy of its output, the shared
+ * projection held fixed.  With t = scale[p] x[r] a[p]^T and
+ * u = scale[p] dy[r] b[p]:
+ *   dx[r] = dy[r] w + u a[p] (nullable: not computed),
+ *   da[p] = sum u^T x[r], db[p] = sum dy[r]^T t over the rows of adapter p
+ * (device, fp32, laid out as a and b; zeros for an adapter without rows).
+ * The sums are taken in a fixed order.  Errors as above. */
+int nsc_adapter_backward(const nsc_adapter_desc* desc, const void* x, const void* dy,
+                         const void* w, const void* a, const void* b, const float* scale,
+                         const int32_t* ids, const int32_t* count, int64_t max_rows, void* dx,
+                         float* da, float* db, void* ws, size_t ws_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

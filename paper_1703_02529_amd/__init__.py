@@ -19,6 +19,8 @@ NSC_REF_PREV, NSC_REF_FIXED = 0, 1
 NSC_METRIC_MSE, NSC_METRIC_SAD, NSC_METRIC_NRMSE, NSC_METRIC_PSNR = 0, 1, 2, 3
 NSC_F32, NSC_BF16, NSC_BF16_PAIRS = 0, 1, 2
 NSC_MAX_CONV = 8
+NSC_T_F32, NSC_T_BF16, NSC_T_F16 = 0, 1, 2
+NSC_ACT_NONE, NSC_ACT_RELU, NSC_ACT_SILU = 0, 1, 2
 
 _i32, _i64, _u32, _dbl = ctypes.c_int32, ctypes.c_int64, ctypes.c_uint32, ctypes.c_double
 _vp, _sz = ctypes.c_void_p, ctypes.c_size_t
@@ -54,6 +56,16 @@ class FrameOutputs(ctypes.Structure):
 class SweepCfg(ctypes.Structure):
     _fields_ = [("ref_mode", _i32), ("delta", _i32), ("fp_target", _dbl), ("fn_target", _dbl),
                 ("t_mse", _dbl), ("t_snn", _dbl), ("t_full", _dbl)]
+
+
+class NormDesc(ctypes.Structure):
+    _fields_ = [("h", _i32), ("w", _i32), ("c", _i32), ("groups", _i32), ("act", _i32),
+                ("dtype", _i32), ("eps", ctypes.c_float), ("x_stride", _i64), ("y_stride", _i64)]
+
+
+class AdapterDesc(ctypes.Structure):
+    _fields_ = [("k", _i32), ("d", _i32), ("rank", _i32), ("n_adapters", _i32), ("dtype", _i32),
+                ("x_stride", _i64), ("y_stride", _i64)]
 
 
 # nsc_sweep_row, as numpy reads it from the bytes of the rows buffer
@@ -109,6 +121,16 @@ def lib() -> ctypes.CDLL:
             "nsc_group_workspace_bytes": (ctypes.c_int, [_vp, _i64, _vp]),
             "nsc_group_run": (ctypes.c_int, [_vp, _vp, _i64, _i64, _vp, _vp, _sz, _vp, _vp, _vp,
                                              _vp, _vp, _vp]),
+            "nsc_norm_check": (ctypes.c_int, [_vp]),
+            "nsc_group_norm_workspace_bytes": (ctypes.c_int, [_vp, _i64, _i32, _vp]),
+            "nsc_group_norm": (ctypes.c_int, [_vp, _vp, _vp, _vp, _vp, _i64, _vp, _vp, _vp, _sz,
+                                              _vp]),
+            "nsc_group_norm_backward": (ctypes.c_int, [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _i64,
+                                                       _vp, _vp, _vp, _vp, _sz, _vp]),
+            "nsc_adapter_check": (ctypes.c_int, [_vp]),
+            "nsc_adapter_workspace_bytes": (ctypes.c_int, [_vp, _i64, _i32, _vp]),
+            "nsc_adapter_project": (ctypes.c_int, [_vp] * 9 + [_i64, _vp, _vp, _sz, _vp]),
+            "nsc_adapter_backward": (ctypes.c_int, [_vp] * 9 + [_i64] + [_vp] * 4 + [_sz, _vp]),
         }
         for name, (res, args) in sig.items():
             fn = getattr(L, name)
@@ -438,3 +460,150 @@ def nsc_threshold_sweep(cfg: SweepCfg, score, conf, truth, deltas, rows, best, s
     _check(lib().nsc_threshold_sweep(ctypes.byref(cfg), _ptr(score), _ptr(conf), _ptr(truth), n,
                                      _ptr(deltas), n_t, _ptr(rows), _ptr(best), _stream(stream)),
            "nsc_threshold_sweep")
+
+
+# ------------------------------------------------------------ single layers
+
+def make_norm_desc(h, w, c, groups, act=NSC_ACT_NONE, dtype=NSC_T_F32, eps=1e-5, x_stride=None,
+                   y_stride=None) -> NormDesc:
+    """Strides in elements between images (default: adjacent)."""
+    e = h * w * c
+    return NormDesc(h, w, c, groups, act, dtype, eps, e if x_stride is None else x_stride,
+                    e if y_stride is None else y_stride)
+
+
+def make_adapter_desc(k, d, rank, n_adapters, dtype=NSC_T_F32, x_stride=None,
+                      y_stride=None) -> AdapterDesc:
+    """Strides in elements between rows (default: adjacent)."""
+    return AdapterDesc(k, d, rank, n_adapters, dtype, k if x_stride is None else x_stride,
+                       d if y_stride is None else y_stride)
+
+
+def _layer_ptrs(stream, *tensors):
+    """The tensors' pointers; all of them must be on the stream's device and
+    that device the current one (the library launches there)."""
+    import torch
+    s = stream if stream is not None else torch.cuda.current_stream()
+    for t in tensors:
+        if t is not None and t.is_cuda and t.device != s.device:
+            raise ValueError(f"tensor on {t.device}, stream on {s.device}")
+    if s.device.index != torch.cuda.current_device():
+        raise ValueError(f"the stream's device {s.device} is not the current one")
+    return [_ptr(t) for t in tensors]
+
+
+def _hold(what, t, dtype, numel):
+    """t must hold `numel` elements of the type: the library sees only its pointer."""
+    if t is not None and (t.dtype != dtype or t.numel() < numel):
+        raise ValueError(f"{what}: {numel} elements of {dtype} expected, got {t.numel()} of "
+                         f"{t.dtype}")
+
+
+def _elem(dtype):
+    import torch
+    return {NSC_T_F32: torch.float32, NSC_T_BF16: torch.bfloat16, NSC_T_F16: torch.float16}[dtype]
+
+
+def _span(n, stride, width):
+    """Elements that n rows `stride` apart reach."""
+    return (n - 1) * stride + width if n > 0 else 0
+
+
+def nsc_norm_check(desc: NormDesc) -> int:
+    return lib().nsc_norm_check(ctypes.byref(desc))
+
+
+def nsc_group_norm_workspace_bytes(desc: NormDesc, max_count: int, backward: bool = False) -> int:
+    b = _sz()
+    _check(lib().nsc_group_norm_workspace_bytes(ctypes.byref(desc), max_count, int(backward),
+                                                ctypes.byref(b)), "nsc_group_norm_workspace_bytes")
+    return b.value
+
+
+def nsc_group_norm(desc: NormDesc, x, gamma, beta, y, ws, max_count, stats=None, count=None,
+                   stream=None):
+    import torch
+    _check(nsc_norm_check(desc), "nsc_group_norm")
+    t, e = _elem(desc.dtype), desc.h * desc.w * desc.c
+    _hold("x", x, t, _span(max_count, desc.x_stride, e))
+    _hold("y", y, t, _span(max_count, desc.y_stride, e))
+    _hold("gamma", gamma, torch.float32, desc.c)
+    _hold("beta", beta, torch.float32, desc.c)
+    _hold("stats", stats, torch.float32, 2 * max_count * desc.groups)
+    _hold("count", count, torch.int32, 1)
+    x, gamma, beta, count, y, stats, w = _layer_ptrs(stream, x, gamma, beta, count, y, stats, ws)
+    _check(lib().nsc_group_norm(ctypes.byref(desc), x, gamma, beta, count, max_count, y, stats, w,
+                                ws.numel() * ws.element_size() if ws is not None else 0,
+                                _stream(stream)), "nsc_group_norm")
+
+
+def nsc_group_norm_backward(desc: NormDesc, x, dy, gamma, beta, stats, dx, dgamma, dbeta, ws,
+                            max_count, count=None, stream=None):
+    import torch
+    _check(nsc_norm_check(desc), "nsc_group_norm_backward")
+    t, e = _elem(desc.dtype), desc.h * desc.w * desc.c
+    for what, v, stride in (("x", x, desc.x_stride), ("dx", dx, desc.x_stride),
+                            ("dy", dy, desc.y_stride)):
+        _hold(what, v, t, _span(max_count, stride, e))
+    for what, v in (("gamma", gamma), ("beta", beta), ("dgamma", dgamma), ("dbeta", dbeta)):
+        _hold(what, v, torch.float32, desc.c)
+    _hold("stats", stats, torch.float32, 2 * max_count * desc.groups)
+    _hold("count", count, torch.int32, 1)
+    p = _layer_ptrs(stream, x, dy, gamma, beta, stats, count, dx, dgamma, dbeta, ws)
+    _check(lib().nsc_group_norm_backward(ctypes.byref(desc), *p[:6], max_count, *p[6:],
+                                         ws.numel() * ws.element_size() if ws is not None else 0,
+                                         _stream(stream)), "nsc_group_norm_backward")
+
+
+def nsc_adapter_check(desc: AdapterDesc) -> int:
+    return lib().nsc_adapter_check(ctypes.byref(desc))
+
+
+def nsc_adapter_workspace_bytes(desc: AdapterDesc, max_rows: int, backward: bool = False) -> int:
+    b = _sz()
+    _check(lib().nsc_adapter_workspace_bytes(ctypes.byref(desc), max_rows, int(backward),
+                                             ctypes.byref(b)), "nsc_adapter_workspace_bytes")
+    return b.value
+
+
+def _hold_adapters(desc, w, a, b, scale, ids, count, max_rows):
+    import torch
+    t = _elem(desc.dtype)
+    _hold("w", w, t, desc.k * desc.d)
+    _hold("a", a, t, desc.n_adapters * desc.rank * desc.k)
+    _hold("b", b, t, desc.n_adapters * desc.rank * desc.d)
+    _hold("scale", scale, torch.float32, desc.n_adapters)
+    _hold("ids", ids, torch.int32, max_rows)
+    _hold("count", count, torch.int32, 1)
+
+
+def nsc_adapter_project(desc: AdapterDesc, x, w, bias, a, b, scale, ids, y, ws, max_rows,
+                        count=None, stream=None):
+    import torch
+    _check(nsc_adapter_check(desc), "nsc_adapter_project")
+    t = _elem(desc.dtype)
+    _hold("x", x, t, _span(max_rows, desc.x_stride, desc.k))
+    _hold("y", y, t, _span(max_rows, desc.y_stride, desc.d))
+    _hold("bias", bias, torch.float32, desc.d)
+    _hold_adapters(desc, w, a, b, scale, ids, count, max_rows)
+    p = _layer_ptrs(stream, x, w, bias, a, b, scale, ids, count, y, ws)
+    _check(lib().nsc_adapter_project(ctypes.byref(desc), *p[:8], max_rows, *p[8:],
+                                     ws.numel() * ws.element_size() if ws is not None else 0,
+                                     _stream(stream)), "nsc_adapter_project")
+
+
+def nsc_adapter_backward(desc: AdapterDesc, x, dy, w, a, b, scale, ids, dx, da, db, ws, max_rows,
+                         count=None, stream=None):
+    import torch
+    _check(nsc_adapter_check(desc), "nsc_adapter_backward")
+    t = _elem(desc.dtype)
+    _hold("x", x, t, _span(max_rows, desc.x_stride, desc.k))
+    _hold("dx", dx, t, _span(max_rows, desc.x_stride, desc.k))
+    _hold("dy", dy, t, _span(max_rows, desc.y_stride, desc.d))
+    _hold("da", da, torch.float32, desc.n_adapters * desc.rank * desc.k)
+    _hold("db", db, torch.float32, desc.n_adapters * desc.rank * desc.d)
+    _hold_adapters(desc, w, a, b, scale, ids, count, max_rows)
+    p = _layer_ptrs(stream, x, dy, w, a, b, scale, ids, count, dx, da, db, ws)
+    _check(lib().nsc_adapter_backward(ctypes.byref(desc), *p[:8], max_rows, *p[8:],
+                                      ws.numel() * ws.element_size() if ws is not None else 0,
+                                      _stream(stream)), "nsc_adapter_backward")

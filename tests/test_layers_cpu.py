@@ -1,0 +1,162 @@
+"""Host-side checks of the single layers (nsc_group_norm, nsc_adapter_project
+and their gradients): descriptions, sizes and refusals, without GPU calls."""
+import ctypes
+import math
+
+import pytest
+
+import paper_1703_02529_amd as nsc
+
+P = 4096  # a non-null, aligned address that no refused call reads
+
+
+def _norm(**kw):
+    base = dict(h=25, w=25, c=64, groups=8, act=nsc.NSC_ACT_RELU, dtype=nsc.NSC_T_BF16)
+    base.update(kw)
+    return nsc.make_norm_desc(**base)
+
+
+@pytest.mark.parametrize("kw", [dict(), dict(h=1, w=1, c=1, groups=1), dict(groups=64),
+                                dict(c=45, groups=5), dict(x_stride=25 * 25 * 64 + 3),
+                                dict(c=1024, groups=1), dict(c=65536, groups=64),
+                                dict(h=4096, w=4096, c=8, groups=1)])
+def test_norm_descriptions_that_hold(kw):
+    assert nsc.nsc_norm_check(_norm(**kw)) == 0, nsc.last_error()
+
+
+@pytest.mark.parametrize("kw,code", [
+    (dict(h=0), nsc.NSC_E_SHAPE), (dict(w=-1), nsc.NSC_E_SHAPE), (dict(c=0), nsc.NSC_E_SHAPE),
+    (dict(h=4097, w=4096), nsc.NSC_E_SHAPE), (dict(c=65537, groups=65537), nsc.NSC_E_SHAPE),
+    (dict(groups=0), nsc.NSC_E_SHAPE), (dict(groups=7), nsc.NSC_E_SHAPE),
+    (dict(groups=128), nsc.NSC_E_SHAPE), (dict(c=2048, groups=1), nsc.NSC_E_SHAPE),
+    (dict(act=3), nsc.NSC_E_INVAL), (dict(act=-1), nsc.NSC_E_INVAL),
+    (dict(dtype=3), nsc.NSC_E_DTYPE), (dict(dtype=-1), nsc.NSC_E_DTYPE),
+    (dict(eps=0.0), nsc.NSC_E_INVAL), (dict(eps=-1.0), nsc.NSC_E_INVAL),
+    (dict(eps=math.nan), nsc.NSC_E_INVAL), (dict(eps=math.inf), nsc.NSC_E_INVAL),
+    (dict(x_stride=25 * 25 * 64 - 1), nsc.NSC_E_INVAL),
+    (dict(y_stride=0), nsc.NSC_E_INVAL), (dict(x_stride=2 ** 41), nsc.NSC_E_INVAL),
+])
+def test_norm_descriptions_that_are_refused(kw, code):
+    assert nsc.nsc_norm_check(_norm(**kw)) == code
+    assert nsc.last_error() != ""
+
+
+def _norm_fwd(d, x=P, gamma=P, beta=P, count=None, n=4, y=P, stats=None, ws=P, ws_bytes=1 << 40):
+    return nsc.lib().nsc_group_norm(ctypes.byref(d), x, gamma, beta, count, n, y, stats, ws,
+                                    ws_bytes, None)
+
+
+def _norm_bwd(d, x=P, dy=P, gamma=P, beta=P, stats=P, n=4, dx=P, dgamma=P, dbeta=P, ws=P,
+              ws_bytes=1 << 40):
+    return nsc.lib().nsc_group_norm_backward(ctypes.byref(d), x, dy, gamma, beta, stats, None, n,
+                                             dx, dgamma, dbeta, ws, ws_bytes, None)
+
+
+def test_norm_calls_are_refused_on_the_host():
+    d = _norm()
+    for kw in (dict(x=None), dict(gamma=None), dict(beta=None), dict(y=None), dict(n=-1),
+               dict(n=2 ** 31), dict(x=P + 1), dict(y=P + 1), dict(gamma=P + 2),
+               dict(beta=P + 1), dict(stats=P + 4), dict(count=P + 2)):
+        assert _norm_fwd(d, **kw) == nsc.NSC_E_INVAL, kw
+    # in place only with equal strides
+    assert _norm_fwd(_norm(y_stride=2 * 25 * 25 * 64)) == nsc.NSC_E_INVAL
+    assert _norm_fwd(d, n=0, x=None, gamma=None, beta=None, y=None) == 0
+    for kw in (dict(x=None), dict(dy=None), dict(gamma=None), dict(beta=None), dict(stats=None),
+               dict(dx=None), dict(dgamma=None), dict(dbeta=None), dict(n=-1), dict(dy=P + 1),
+               dict(stats=P + 4), dict(dgamma=P + 2)):
+        assert _norm_bwd(d, **kw) == nsc.NSC_E_INVAL, kw
+    need = nsc.nsc_group_norm_workspace_bytes(d, 4, backward=True)
+    assert need > 0
+    for kw in (dict(ws=None), dict(ws=P + 128), dict(ws_bytes=need - 1)):
+        assert _norm_bwd(d, **kw) == nsc.NSC_E_WORKSPACE, kw
+    assert nsc.lib().nsc_group_norm(None, P, P, P, None, 1, P, None, P, 0, None) == nsc.NSC_E_INVAL
+
+
+def test_norm_workspace_sizes():
+    d = _norm()
+    sizes = [nsc.nsc_group_norm_workspace_bytes(d, n, backward=True) for n in (0, 1, 100, 10000)]
+    assert sizes == sorted(sizes)
+    for bad in (-1, 2 ** 31):
+        with pytest.raises(nsc.NscError):
+            nsc.nsc_group_norm_workspace_bytes(d, bad)
+    with pytest.raises(nsc.NscError):
+        nsc.nsc_group_norm_workspace_bytes(_norm(groups=7), 1)
+    assert nsc.lib().nsc_group_norm_workspace_bytes(ctypes.byref(d), 1, 0, None) == nsc.NSC_E_INVAL
+    b = ctypes.c_size_t()
+    assert nsc.lib().nsc_group_norm_workspace_bytes(ctypes.byref(d), 1, 2,
+                                                    ctypes.byref(b)) == nsc.NSC_E_INVAL
+
+
+def _adapter(**kw):
+    base = dict(k=4608, d=128, rank=8, n_adapters=24, dtype=nsc.NSC_T_BF16)
+    base.update(kw)
+    return nsc.make_adapter_desc(**base)
+
+
+@pytest.mark.parametrize("kw", [dict(), dict(k=1, d=1, rank=1, n_adapters=1), dict(rank=128),
+                                dict(n_adapters=65535), dict(x_stride=5000, y_stride=129)])
+def test_adapter_descriptions_that_hold(kw):
+    assert nsc.nsc_adapter_check(_adapter(**kw)) == 0, nsc.last_error()
+
+
+@pytest.mark.parametrize("kw,code", [
+    (dict(k=0), nsc.NSC_E_SHAPE), (dict(d=0), nsc.NSC_E_SHAPE), (dict(k=2 ** 24 + 1), nsc.NSC_E_SHAPE),
+    (dict(d=2 ** 24 + 1), nsc.NSC_E_SHAPE), (dict(rank=0), nsc.NSC_E_SHAPE),
+    (dict(rank=129), nsc.NSC_E_SHAPE), (dict(n_adapters=0), nsc.NSC_E_INVAL),
+    (dict(n_adapters=65536), nsc.NSC_E_INVAL), (dict(dtype=3), nsc.NSC_E_DTYPE),
+    (dict(x_stride=4607), nsc.NSC_E_INVAL), (dict(y_stride=127), nsc.NSC_E_INVAL),
+    (dict(x_stride=2 ** 32), nsc.NSC_E_INVAL),
+])
+def test_adapter_descriptions_that_are_refused(kw, code):
+    assert nsc.nsc_adapter_check(_adapter(**kw)) == code
+    assert nsc.last_error() != ""
+
+
+def _project(d, x=P, w=P, bias=None, a=P, b=P, scale=P, ids=P, n=4, y=P, ws=P, ws_bytes=1 << 40):
+    return nsc.lib().nsc_adapter_project(ctypes.byref(d), x, w, bias, a, b, scale, ids, None, n, y,
+                                         ws, ws_bytes, None)
+
+
+def _project_bwd(d, x=P, dy=P, w=P, a=P, b=P, scale=P, ids=P, n=4, dx=None, da=P, db=P, ws=P,
+                 ws_bytes=1 << 40):
+    return nsc.lib().nsc_adapter_backward(ctypes.byref(d), x, dy, w, a, b, scale, ids, None, n, dx,
+                                          da, db, ws, ws_bytes, None)
+
+
+def test_adapter_calls_are_refused_on_the_host():
+    d = _adapter()
+    for kw in (dict(x=None), dict(w=None), dict(a=None), dict(b=None), dict(scale=None),
+               dict(ids=None), dict(y=None), dict(n=-1), dict(n=2 ** 31), dict(x=P + 1),
+               dict(bias=P + 2), dict(scale=P + 1), dict(ids=P + 2), dict(y=P + 1)):
+        assert _project(d, **kw) == nsc.NSC_E_INVAL, kw
+    need = nsc.nsc_adapter_workspace_bytes(d, 4)
+    for kw in (dict(ws=None), dict(ws=P + 16), dict(ws_bytes=need - 1)):
+        assert _project(d, **kw) == nsc.NSC_E_WORKSPACE, kw
+    assert _project(d, n=0, x=None, ws=None, ws_bytes=0) == 0
+    for kw in (dict(x=None), dict(dy=None), dict(w=None), dict(a=None), dict(b=None),
+               dict(scale=None), dict(ids=None), dict(da=None), dict(db=None), dict(n=-1),
+               dict(dy=P + 1), dict(da=P + 2)):
+        assert _project_bwd(d, **kw) == nsc.NSC_E_INVAL, kw
+    need = nsc.nsc_adapter_workspace_bytes(d, 4, backward=True)
+    for kw in (dict(ws=None), dict(ws=P + 16), dict(ws_bytes=need - 1)):
+        assert _project_bwd(d, **kw) == nsc.NSC_E_WORKSPACE, kw
+    with pytest.raises(nsc.NscError):
+        nsc.nsc_adapter_workspace_bytes(d, -1)
+
+
+def test_the_binding_refuses_host_tensors_and_short_buffers():
+    torch = pytest.importorskip("torch")
+    d = _adapter()
+    x = torch.zeros(4 * 4608, dtype=torch.bfloat16)
+    with pytest.raises(ValueError, match="x:"):
+        nsc.nsc_adapter_project(d, x[:-1], x, None, x, x, x, x, x, x, 4)
+    with pytest.raises(ValueError, match="x:"):
+        nsc.nsc_adapter_project(d, x.float(), x, None, x, x, x, x, x, x, 4)
+    with pytest.raises(nsc.NscError):
+        nsc.nsc_adapter_project(_adapter(rank=0), x, x, None, x, x, x, x, x, x, 4)
+    n = _norm()
+    m = torch.zeros(25 * 25 * 64, dtype=torch.bfloat16)
+    with pytest.raises(ValueError, match="x:"):
+        nsc.nsc_group_norm(n, m, m, m, m, None, 2)
+    with pytest.raises(ValueError, match="gamma:"):
+        nsc.nsc_group_norm(n, m, m, m, m, None, 1)
