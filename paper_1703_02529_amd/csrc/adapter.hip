@@ -84,25 +84,33 @@ struct AdapterArgs {
   const void* b;            // [n_adapters][d][rank]
   const float* scale;
   const int32_t* ids;
+  const int32_t* rows;      // the row at each position (k_adapter_list); null: itself
   const int32_t* count;     // nullable
   int64_t max_rows;
   int64_t in_stride, out_stride;
   void* out;
-  float* t;                 // [rows][rp] rank-wide rows
+  float* t;                 // [t_parts][max_rows][rp] rank-wide rows, by position
+  float* part;              // the product's partial sums (parts > 1)
   int32_t k, d, rank, rp, n_adapters;
+  int32_t t_parts;          // parts of the rank-wide rows' reduction
+  int32_t parts;            // parts of the product's reduction
+  int32_t b4;               // four values of a row of b are one aligned load
+  int32_t out4;             // four neighbouring outputs are one aligned store
 };
 
 __device__ __forceinline__ int64_t live_rows(const AdapterArgs& a) {
   int64_t n = a.count ? *a.count : a.max_rows;
   return n < a.max_rows ? n : a.max_rows;
 }
-// The adapter of row r, INT_MAX without one.
-__device__ __forceinline__ int row_adapter(const AdapterArgs& a, int64_t r, int64_t n) {
-  if (r >= n) return INT_MAX;
-  const int p = a.ids[r];
+// The row at a position below n, and its adapter (INT_MAX without one).
+__device__ __forceinline__ int64_t row_at(const AdapterArgs& a, int64_t pos) {
+  return a.rows ? a.rows[pos] : pos;
+}
+__device__ __forceinline__ int adapter_of(const AdapterArgs& a, int64_t row) {
+  const int p = a.ids[row];
   return p >= 0 && p < a.n_adapters ? p : INT_MAX;
 }
-// The smallest adapter above p among a wave's lanes (INT_MAX: none).
+// The smallest adapter above p among 16 rows (INT_MAX: none).
 __device__ __forceinline__ int next_adapter(int mine, int p) {
   int v = mine > p ? mine : INT_MAX;
 #pragma unroll
@@ -110,23 +118,30 @@ __device__ __forceinline__ int next_adapter(int mine, int p) {
   return __builtin_amdgcn_readfirstlane(v);
 }
 
-// Rank-wide rows: a workgroup per 16 rows, whose waves split the reduction and
-// add their sums through LDS.  B = false: t = scale x a^T over k; B = true:
-// u = scale dy b over d, whose values lie rank apart.
-constexpr int kDownWaves = 8;
+// Rank-wide rows of 16 positions: a workgroup per (tile, part of the
+// reduction), whose waves split the part and add their sums through LDS.  A
+// lane keeps the products of its own row's adapter.  B = false: t = scale x a^T
+// over k; B = true: u = scale dy b over d, whose values lie rank apart.
+constexpr int kDownWaves = 4;
+constexpr int kDownUnroll = 4;  // steps whose loads are in flight together
 
 template <typename T, bool VEC, bool B>
 __global__ void __launch_bounds__(64 * kDownWaves) k_adapter_down(AdapterArgs a) {
   using M = Mma<T>;
+  constexpr int KS = B ? 16 : M::KS;
   __shared__ f32x4 red[kDownWaves][64];
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int m = lane & 15, g = lane >> 4;
   const int64_t n = live_rows(a);
   const int len = B ? a.d : a.k;
-  for (int64_t row0 = blockIdx.x * 16ll; row0 < n; row0 += gridDim.x * 16ll) {
-    const int64_t row = row0 + m < n ? row0 + m : n - 1;
-    const int mine = row_adapter(a, row0 + m, n);
+  const int steps = (len + KS - 1) / KS, part = blockIdx.y * kDownWaves + wave;
+  const int s0 = (int)((int64_t)part * steps / (a.t_parts * kDownWaves));
+  const int s1 = (int)((int64_t)(part + 1) * steps / (a.t_parts * kDownWaves));
+  for (int64_t pos0 = blockIdx.x * 16ll; pos0 < n; pos0 += gridDim.x * 16ll) {
+    const bool in = pos0 + m < n;
+    const int64_t row = row_at(a, in ? pos0 + m : n - 1);
+    const int mine = in ? adapter_of(a, row) : INT_MAX;
     const T* x = static_cast<const T*>(a.x) + row * a.in_stride;
     for (int j0 = 0; j0 < a.rp; j0 += 16) {
       f32x4 out = {0.f, 0.f, 0.f, 0.f};
@@ -135,8 +150,8 @@ __global__ void __launch_bounds__(64 * kDownWaves) k_adapter_down(AdapterArgs a)
         f32x4 acc = {0.f, 0.f, 0.f, 0.f};
         if constexpr (B) {
           const T* b = static_cast<const T*>(a.b) + (int64_t)p * a.d * a.rank + j;
-          for (int k0 = wave * 16; k0 < len; k0 += 16 * kDownWaves) {
-            const int k = k0 + 4 * g;
+          for (int s = s0; s < s1; ++s) {
+            const int k = s * KS + 4 * g;
             f32x4 bv;
 #pragma unroll
             for (int e = 0; e < 4; ++e)
@@ -145,140 +160,320 @@ __global__ void __launch_bounds__(64 * kDownWaves) k_adapter_down(AdapterArgs a)
           }
         } else {
           const T* ar = static_cast<const T*>(a.a) + ((int64_t)p * a.rank + j) * a.k;
-          for (int k0 = wave * M::KS; k0 < len; k0 += M::KS * kDownWaves) {
-            const int k = k0 + M::E * g;
-            const uint4 av = load_frag<T, VEC>(ar + k, j < a.rank ? len - k : 0);
-            acc = M::mma(av, load_frag<T, VEC>(x + k, len - k), acc);
+          for (int s = s0; s < s1; s += kDownUnroll) {
+            uint4 av[kDownUnroll], xv[kDownUnroll];
+#pragma unroll
+            for (int u = 0; u < kDownUnroll; ++u) {
+              const int k = (s + u) * KS + M::E * g;
+              const int left = s + u < s1 ? len - k : 0;
+              av[u] = load_frag<T, VEC>(ar + k, j < a.rank ? left : 0);
+              xv[u] = load_frag<T, VEC>(x + k, left);
+            }
+#pragma unroll
+            for (int u = 0; u < kDownUnroll; ++u) acc = M::mma(av[u], xv[u], acc);
           }
         }
-        __syncthreads();  // red is read before it is written again
-        red[wave][lane] = acc;
-        __syncthreads();
-        if (wave == 0) {
-#pragma unroll
-          for (int w = 1; w < kDownWaves; ++w) acc += red[w][lane];
-          if (mine == p) out = acc * a.scale[p];
-        }
+        if (mine == p) out = acc * a.scale[p];
       }
-      if (wave == 0 && row0 + m < n)
-        *reinterpret_cast<f32x4*>(a.t + row * a.rp + j0 + 4 * g) = out;
+      __syncthreads();  // red is read before it is written again
+      red[wave][lane] = out;
+      __syncthreads();
+      if (wave == 0 && in) {
+#pragma unroll
+        for (int w = 1; w < kDownWaves; ++w) out += red[w][lane];
+        *reinterpret_cast<f32x4*>(a.t + ((int64_t)blockIdx.y * a.max_rows + pos0 + m) * a.rp + j0 +
+                                  4 * g) = out;
+      }
     }
   }
 }
 
-// The shared product with the rank-wide rows' in its epilogue: 64 x 64 tiles
-// of (outputs, rows), 128 bytes of the reduction at a time through LDS, whose
-// 16-byte chunks c of row r lie at chunk c ^ (r & 7).  TR = false: outputs d
-// from x w^T + t b^T; TR = true: outputs k from dy w + u a, the weights
-// transposed on their way into LDS.
-constexpr int kTile = 64;
-
-template <typename T, bool VEC, bool TR>
-__global__ void __launch_bounds__(256) k_adapter_gemm(AdapterArgs a) {
+// The shared product with the rank-wide rows' in its epilogue, in tiles of TN
+// outputs x TM rows.  The reduction goes through LDS 128 bytes of a row at a
+// time, copied there directly from memory while the previous 128 are
+// multiplied; what lies behind the reduction's end, or is not aligned to 16
+// bytes, is loaded through registers and filled with zeros.
+// TR = false: outputs d from x w^T + t b^T.  TR = true: outputs k from
+// dy w + u a; the weights' reduction then runs down the columns of w, whose
+// tile keeps its rows in LDS and is transposed as it is read.
+// With parts > 1 the workgroups of a tile share its reduction and write their
+// sums, which k_adapter_join adds in order before the same epilogue.
+template <typename T, bool TR, int TN, int TM>
+struct Gemm {
   using M = Mma<T>;
-  constexpr int E = M::E, BK = 2 * M::KS;  // values per 128 bytes
-  __shared__ uint4 wl[kTile][8], xl[kTile][8];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  static constexpr int E = M::E, BK = 2 * M::KS;      // values per 16 and per 128 bytes
+  static constexpr int WM = TM >= 64 ? 2 : 1;         // waves along the rows
+  static constexpr int WN = 4 / WM;                   // and along the outputs
+  static constexpr int NI = TN / WN / 16, NJ = TM / WM / 16;
+  static constexpr int WCH = TN * BK * sizeof(T) / 16, XCH = TM * 8;  // 16-byte chunks of a tile
+  static constexpr int RCH = TR ? TN / E : 8;         // chunks of a row of the weights' tile
+  static constexpr size_t kLds = 2 * (WCH + XCH) * 16;
+
+  // Chunk c of row r lies at chunk slot(r, c) of its row, so that the lanes of
+  // a read fall on different banks: x and w by rows (16 lanes read one chunk
+  // of 16 rows), and w transposed (16-bit: 32-byte blocks of rows 8 g + 0..3
+  // of 2 lane groups at once; 32-bit: 64-byte blocks of rows 4 g of 4).
+  static __device__ __forceinline__ int xslot(int r, int c) { return c ^ (r & 7); }
+  static __device__ __forceinline__ int wslot(int r, int c) {
+    if constexpr (!TR) return c ^ (r & 7);
+    if constexpr (sizeof(T) == 2) return c ^ ((((r & 3) | ((r >> 1) & 4)) << 1) & (RCH - 1));
+    return c ^ ((((r >> 2) & 3) << 2) & (RCH - 1));
+  }
+  // The weights' fragment of outputs o .. o + 15 at step s.
+  static __device__ __forceinline__ uint4 wfrag(const uint4* wl, int o, int s, int m, int g) {
+    if constexpr (!TR) {
+      return wl[(o + m) * 8 + xslot(o + m, 4 * s + g)];
+    } else if constexpr (sizeof(T) == 2) {
+      uint2 h[2];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int r = s * 32 + 8 * g + 4 * i + (m >> 2), c = (o >> 3) + ((m >> 1) & 1);
+        typedef short s16x4 __attribute__((ext_vector_type(4)));
+        const char* at = reinterpret_cast<const char*>(wl + r * RCH + wslot(r, c)) + (m & 1) * 8;
+        h[i] = __builtin_bit_cast(
+            uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                       (__attribute__((address_space(3))) s16x4*)(at)));
+      }
+      return make_uint4(h[0].x, h[0].y, h[1].x, h[1].y);
+    } else {
+      f32x4 v;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int r = s * 16 + 4 * g + e;
+        v[e] = reinterpret_cast<const float*>(wl + r * RCH + wslot(r, (o + m) >> 2))[m & 3];
+      }
+      return __builtin_bit_cast(uint4, v);
+    }
+  }
+};
+
+// 16 bytes per lane from memory straight to LDS, at the wave's lds + 16 * lane.
+__device__ __forceinline__ void copy_to_lds(const void* from, void* lds) {
+  __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from,
+                                   (__attribute__((address_space(3))) void*)lds, 16, 0, 0);
+}
+
+template <typename T, bool TR, int NI, int NJ>
+__device__ __forceinline__ void adapter_epilogue(const AdapterArgs& a, f32x4 (&acc)[NI][NJ],
+                                                 int o0, int64_t pos0, int64_t n, int m, int g) {
+  const int outs = TR ? a.k : a.d;
+#pragma unroll
+  for (int j = 0; j < NJ; ++j) {  // 16 positions
+    const int64_t pos = pos0 + j * 16 + m;
+    const int64_t row = pos < n ? row_at(a, pos) : 0;
+    const int mine = pos < n ? adapter_of(a, row) : INT_MAX;
+    for (int p = next_adapter(mine, -1); p != INT_MAX; p = next_adapter(mine, p)) {
+      f32x4 add[NI];
+#pragma unroll
+      for (int i = 0; i < NI; ++i) add[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+      for (int q0 = 0; q0 < a.rp; q0 += 16) {
+        const int q = q0 + 4 * g;
+        f32x4 tv = {0.f, 0.f, 0.f, 0.f};
+        if (mine == p)
+          for (int h = 0; h < a.t_parts; ++h)
+            tv += *reinterpret_cast<const f32x4*>(a.t + (h * a.max_rows + pos) * a.rp + q);
+#pragma unroll
+        for (int i = 0; i < NI; ++i) {
+          const int o = o0 + i * 16 + m;
+          f32x4 bv = {0.f, 0.f, 0.f, 0.f};
+          if (o < outs) {
+            if constexpr (TR) {
+              const T* ap = static_cast<const T*>(a.a) + (int64_t)p * a.rank * a.k + o;
+#pragma unroll
+              for (int e = 0; e < 4; ++e)
+                if (q + e < a.rank) bv[e] = (float)ap[(int64_t)(q + e) * a.k];
+            } else {
+              const T* bp = static_cast<const T*>(a.b) + ((int64_t)p * a.d + o) * a.rank + q;
+              if (a.b4) {
+                if (q < a.rank) {
+                  const Vec<T, 4> v = *reinterpret_cast<const Vec<T, 4>*>(bp);
+#pragma unroll
+                  for (int e = 0; e < 4; ++e) bv[e] = (float)v.e[e];
+                }
+              } else {
+                bv = load4(bp, a.rank - q);
+              }
+            }
+          }
+          add[i] = mma_f32(bv, tv, add[i]);
+        }
+      }
+      if (mine == p) {
+#pragma unroll
+        for (int i = 0; i < NI; ++i) acc[i][j] += add[i];
+      }
+    }
+    if (pos < n) {
+      T* y = static_cast<T*>(a.out) + row * a.out_stride;
+#pragma unroll
+      for (int i = 0; i < NI; ++i) {
+        const int o = o0 + i * 16 + 4 * g;
+        Vec<T, 4> v;
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          v.e[e] = (T)(acc[i][j][e] + (a.bias && o + e < outs ? a.bias[o + e] : 0.0f));
+        if (a.out4) {
+          if (o < outs) *reinterpret_cast<Vec<T, 4>*>(y + o) = v;
+        } else {
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (o + e < outs) y[o + e] = v.e[e];
+        }
+      }
+    }
+  }
+}
+
+template <typename T, bool VEC, bool TR, int TN, int TM>
+__global__ void __launch_bounds__(256) k_adapter_gemm(AdapterArgs a) {
+  using G = Gemm<T, TR, TN, TM>;
+  using M = Mma<T>;
+  constexpr int E = G::E, BK = G::BK, NI = G::NI, NJ = G::NJ;
+  extern __shared__ __align__(16) uint4 lds[];
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int m = lane & 15, g = lane >> 4;
   const int64_t n = live_rows(a);
   const int outs = TR ? a.k : a.d, len = TR ? a.d : a.k;
-  const int o0 = blockIdx.x * kTile, wo = (wave & 1) * 32, wr = (wave >> 1) * 32;
+  const int o0 = blockIdx.x * TN;
+  const int wo = (wave % G::WN) * NI * 16, wr = (wave / G::WN) * NJ * 16;
   const T* w = static_cast<const T*>(a.w);
   const T* xs = static_cast<const T*>(a.x);
-  for (int64_t r0 = blockIdx.y * (int64_t)kTile; r0 < n; r0 += gridDim.y * (int64_t)kTile) {
-    f32x4 acc[2][2];
+  const int blocks = (len + BK - 1) / BK;
+  const int b0 = (int)((int64_t)blockIdx.z * blocks / a.parts);
+  const int b1 = (int)((int64_t)(blockIdx.z + 1) * blocks / a.parts);
+  constexpr int XC = (G::XCH + 255) / 256, WC = G::WCH / 256;  // chunks per thread
+  static_assert(G::WCH % 256 == 0, "whole chunks per thread");
+  for (int64_t pos0 = blockIdx.y * (int64_t)TM; pos0 < n; pos0 += gridDim.y * (int64_t)TM) {
+    f32x4 acc[NI][NJ];
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
+    for (int i = 0; i < NI; ++i)
 #pragma unroll
-      for (int j = 0; j < 2; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-    for (int k0 = 0; k0 < len; k0 += BK) {
-      __syncthreads();
-      for (int c = threadIdx.x; c < kTile * 8; c += 256) {
-        const int r = c >> 3, ch = c & 7, k = k0 + ch * E;
-        const int64_t row = r0 + r < n ? r0 + r : n - 1;
-        xl[r][ch ^ (r & 7)] = load_frag<T, VEC>(xs + row * a.in_stride + k, len - k);
-        if constexpr (!TR) {
-          const int o = o0 + r < outs ? o0 + r : outs - 1;
-          wl[r][ch ^ (r & 7)] = load_frag<T, VEC>(w + (int64_t)o * a.k + k, len - k);
-        }
-      }
-      if constexpr (TR) {
-        for (int c = threadIdx.x; c < kTile * BK; c += 256) {
-          const int o = c % kTile, k = c / kTile;  // lanes along the outputs
-          const bool in = o0 + o < outs && k0 + k < len;
-          reinterpret_cast<T*>(&wl[o][(k / E) ^ (o & 7)])[k % E] =
-              in ? w[(int64_t)(k0 + k) * a.k + o0 + o] : (T)0.0f;
-        }
-      }
-      __syncthreads();
+      for (int j = 0; j < NJ; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    // this thread's chunks: LDS slot c = 256 i + thread holds its row's chunk
+    // slot(row, c), as the slots are their own inverses
+    const T* xp[XC];
+    const T* wp[WC];
 #pragma unroll
-      for (int s = 0; s < 2; ++s) {
-        uint4 av[2], bv[2];
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          const int ro = wo + i * 16 + m, rr = wr + i * 16 + m;
-          av[i] = wl[ro][(4 * s + g) ^ (ro & 7)];
-          bv[i] = xl[rr][(4 * s + g) ^ (rr & 7)];
-        }
-#pragma unroll
-        for (int i = 0; i < 2; ++i)
-#pragma unroll
-          for (int j = 0; j < 2; ++j) acc[i][j] = M::mma(av[i], bv[j], acc[i][j]);
-      }
+    for (int i = 0; i < XC; ++i) {
+      const int c = i * 256 + threadIdx.x, r = c >> 3;
+      const int64_t pos = pos0 + r < n ? pos0 + r : n - 1;
+      xp[i] = xs + row_at(a, pos) * a.in_stride + G::xslot(r, c & 7) * E;
     }
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {  // 16 rows
-      const int64_t row = r0 + wr + j * 16 + m;
-      const int mine = row_adapter(a, row, n);
-      for (int p = next_adapter(mine, -1); p != INT_MAX; p = next_adapter(mine, p)) {
-        f32x4 add[2];
-#pragma unroll
-        for (int i = 0; i < 2; ++i) add[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-        for (int q0 = 0; q0 < a.rp; q0 += 16) {
-          const int q = q0 + 4 * g;
-          f32x4 tv = {0.f, 0.f, 0.f, 0.f};
-          if (mine == p) tv = *reinterpret_cast<const f32x4*>(a.t + row * a.rp + q);
-#pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            const int o = o0 + wo + i * 16 + m;
-            f32x4 bv = {0.f, 0.f, 0.f, 0.f};
-            if (o < outs) {
-              if constexpr (TR) {
-                const T* ap = static_cast<const T*>(a.a) + (int64_t)p * a.rank * a.k + o;
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-                  if (q + e < a.rank) bv[e] = (float)ap[(int64_t)(q + e) * a.k];
-              } else {
-                bv = load4(static_cast<const T*>(a.b) + ((int64_t)p * a.d + o) * a.rank + q,
-                           a.rank - q);
-              }
-            }
-            add[i] = mma_f32(bv, tv, add[i]);
-          }
-        }
-        if (mine == p) {
-#pragma unroll
-          for (int i = 0; i < 2; ++i) acc[i][j] += add[i];
-        }
+    for (int i = 0; i < WC; ++i) {
+      const int c = i * 256 + threadIdx.x, r = c / G::RCH;
+      const int ch = G::wslot(r, c % G::RCH);
+      if constexpr (TR) {
+        const int o = o0 + ch * E < outs ? o0 + ch * E : 0;
+        wp[i] = w + (int64_t)r * a.k + o;
+      } else {
+        const int o = o0 + r < outs ? o0 + r : outs - 1;
+        wp[i] = w + (int64_t)o * a.k + ch * E;
       }
-      if (row < n) {
-        T* y = static_cast<T*>(a.out) + row * a.out_stride;
+    }
+    auto stage = [&](int b, int buf) {
+      uint4* wl = lds + buf * (G::WCH + G::XCH);
+      uint4* xl = wl + G::WCH;
+      const int k0 = b * BK;
+      if (VEC && k0 + BK <= len) {
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          const int o = o0 + wo + i * 16 + 4 * g;
+        for (int i = 0; i < WC; ++i)
+          copy_to_lds(wp[i] + (TR ? (int64_t)k0 * a.k : k0), wl + i * 256 + wave * 64);
 #pragma unroll
-          for (int e = 0; e < 4; ++e)
-            if (o + e < outs)
-              y[o + e] = (T)(acc[i][j][e] + (a.bias ? a.bias[o + e] : 0.0f));
-        }
+        for (int i = 0; i < XC; ++i)
+          if (G::XCH % 256 == 0 || i * 256 + wave * 64 < G::XCH)
+            copy_to_lds(xp[i] + k0, xl + i * 256 + wave * 64);
+        return;
       }
+#pragma unroll
+      for (int i = 0; i < WC; ++i) {
+        const int c = i * 256 + threadIdx.x, r = c / G::RCH;
+        const int ch = G::wslot(r, c % G::RCH);
+        if constexpr (TR)
+          wl[c] = load_frag<T, VEC>(w + (int64_t)(k0 + r) * a.k + o0 + ch * E,
+                                    k0 + r < len ? outs - o0 - ch * E : 0);
+        else
+          wl[c] = load_frag<T, VEC>(wp[i] + k0, len - k0 - ch * E);
+      }
+#pragma unroll
+      for (int i = 0; i < XC; ++i) {
+        const int c = i * 256 + threadIdx.x;
+        if (c < G::XCH) xl[c] = load_frag<T, VEC>(xp[i] + k0, len - k0 - G::xslot(c >> 3, c & 7) * E);
+      }
+    };
+    if (b0 < b1) stage(b0, 0);
+    for (int b = b0; b < b1; ++b) {
+      // this block's copies have landed, and every wave is done with the other buffer
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      __syncthreads();
+      if (b + 1 < b1) stage(b + 1, (b + 1 - b0) & 1);
+      const uint4* wl = lds + ((b - b0) & 1) * (G::WCH + G::XCH);
+      const uint4* xl = wl + G::WCH;
+#pragma unroll
+      for (int s = 0; s < 2; ++s) {
+        uint4 av[NI], bv[NJ];
+#pragma unroll
+        for (int i = 0; i < NI; ++i) av[i] = G::wfrag(wl, wo + i * 16, s, m, g);
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) {
+          const int r = wr + j * 16 + m;
+          bv[j] = xl[r * 8 + G::xslot(r, 4 * s + g)];
+        }
+#pragma unroll
+        for (int i = 0; i < NI; ++i)
+#pragma unroll
+          for (int j = 0; j < NJ; ++j) acc[i][j] = M::mma(av[i], bv[j], acc[i][j]);
+      }
+    }
+    __syncthreads();  // the buffers are read before the next tile's copies
+    if (a.parts > 1) {
+      const int64_t tile = (pos0 / TM) * gridDim.x + blockIdx.x;
+      f32x4* out = reinterpret_cast<f32x4*>(a.part) +
+                   (tile * a.parts + blockIdx.z) * (TN * TM / 4) + wave * NI * NJ * 64 + lane;
+#pragma unroll
+      for (int i = 0; i < NI; ++i)
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) out[(i * NJ + j) * 64] = acc[i][j];
+    } else {
+      adapter_epilogue<T, TR, NI, NJ>(a, acc, o0 + wo, pos0 + wr, n, m, g);
     }
   }
 }
 
-// The rows of each adapter in ascending order: rows[off[p] .. off[p + 1]).  A
-// workgroup per adapter counts the rows of smaller adapters and its own, then
-// writes its own.  Waves take consecutive ranges of the rows.
+// Adds a tile's parts in order, then its epilogue: a workgroup per tile.
+template <typename T, bool TR, int TN, int TM>
+__global__ void __launch_bounds__(256) k_adapter_join(AdapterArgs a) {
+  using G = Gemm<T, TR, TN, TM>;
+  constexpr int NI = G::NI, NJ = G::NJ;
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t n = live_rows(a);
+  for (int64_t pos0 = blockIdx.y * (int64_t)TM; pos0 < n; pos0 += gridDim.y * (int64_t)TM) {
+    const int64_t tile = (pos0 / TM) * gridDim.x + blockIdx.x;
+    const f32x4* in = reinterpret_cast<const f32x4*>(a.part) + tile * a.parts * (TN * TM / 4) +
+                      wave * NI * NJ * 64 + lane;
+    f32x4 acc[NI][NJ];
+#pragma unroll
+    for (int i = 0; i < NI; ++i)
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) acc[i][j] = in[(i * NJ + j) * 64];
+    for (int h = 1; h < a.parts; ++h) {
+      in += TN * TM / 4;
+#pragma unroll
+      for (int i = 0; i < NI; ++i)
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) acc[i][j] += in[(i * NJ + j) * 64];
+    }
+    adapter_epilogue<T, TR, NI, NJ>(a, acc, blockIdx.x * TN + (wave % G::WN) * NI * 16,
+                                    pos0 + (wave / G::WN) * NJ * 16, n, lane & 15, lane >> 4);
+  }
+}
+
+// The rows of each adapter in ascending order: rows[off[p] .. off[p + 1]), and
+// those without one last.  A workgroup per adapter (and one for the rest)
+// counts the rows of smaller adapters and its own, then writes its own.  Waves
+// take consecutive ranges of the rows.
 constexpr int kListWaves = 16;
 
 __global__ void __launch_bounds__(64 * kListWaves) k_adapter_list(AdapterArgs a, int32_t* off,
@@ -288,11 +483,15 @@ __global__ void __launch_bounds__(64 * kListWaves) k_adapter_list(AdapterArgs a,
   const int64_t n = live_rows(a);
   const int64_t per = (n + kListWaves * 64 - 1) / (kListWaves * 64) * 64;
   const int64_t b = wave * per < n ? wave * per : n, e = b + per < n ? b + per : n;
-  for (int p = blockIdx.x; p < a.n_adapters; p += gridDim.x) {
+  for (int p = blockIdx.x; p <= a.n_adapters; p += gridDim.x) {
+    auto of = [&](int64_t r) {
+      const int q = r < e ? a.ids[r] : -1;
+      return q >= 0 && q < a.n_adapters ? q : (r < e ? a.n_adapters : INT_MAX);
+    };
     int32_t lo = 0, eq = 0;
     for (int64_t r = b; r < e; r += 64) {
-      const int mine = r + lane < e ? a.ids[r + lane] : -1;
-      lo += __popcll(__ballot(mine >= 0 && mine < p));
+      const int mine = of(r + lane);
+      lo += __popcll(__ballot(mine < p));
       eq += __popcll(__ballot(mine == p));
     }
     __syncthreads();
@@ -301,20 +500,12 @@ __global__ void __launch_bounds__(64 * kListWaves) k_adapter_list(AdapterArgs a,
       same[wave] = eq;
     }
     __syncthreads();
-    int32_t first = 0, at = 0, all = 0;
+    int32_t at = 0;
 #pragma unroll
-    for (int w = 0; w < kListWaves; ++w) {
-      first += less[w];
-      at += w < wave ? same[w] : 0;
-      all += same[w];
-    }
-    if (threadIdx.x == 0) {
-      off[p] = first;
-      if (p == a.n_adapters - 1) off[a.n_adapters] = first + all;
-    }
-    at += first;
+    for (int w = 0; w < kListWaves; ++w) at += less[w] + (w < wave ? same[w] : 0);
+    if (threadIdx.x == 0) off[p] = at;
     for (int64_t r = b; r < e; r += 64) {
-      const bool mine = r + lane < e && a.ids[r + lane] == p;
+      const bool mine = of(r + lane) == p;
       const uint64_t mask = __ballot(mine);
       if (mine) rows[at + __popcll(mask & ((1ull << lane) - 1))] = (int32_t)(r + lane);
       at += __popcll(mask);
@@ -329,13 +520,14 @@ __global__ void __launch_bounds__(64 * kListWaves) k_adapter_list(AdapterArgs a,
 constexpr int kGradWaves = 8;
 
 struct GradArgs {
-  const float* t;           // u, or t
+  const float* t;           // u, or t: [t_parts][max_rows][rp]
   const void* v;            // x, or dy
   int64_t v_stride;
   const int32_t* off;
   const int32_t* rows;
   float* out;
-  int32_t cols, rank, rp, n_adapters;
+  int64_t max_rows;
+  int32_t cols, rank, rp, n_adapters, t_parts;
 };
 
 template <typename T, bool B>
@@ -358,7 +550,9 @@ __global__ void __launch_bounds__(64 * kGradWaves) k_adapter_grad(GradArgs a) {
           const int32_t at = r + 4 * g + s;
           const bool in = at < e;
           const int64_t row = in ? a.rows[at] : 0;
-          uv[s] = in ? a.t[row * a.rp + j0 + m] : 0.0f;
+          uv[s] = 0.0f;
+          for (int h = 0; in && h < a.t_parts; ++h)
+            uv[s] += a.t[(h * a.max_rows + at) * a.rp + j0 + m];
           const f32x4 v = load4(static_cast<const T*>(a.v) + row * a.v_stride + c,
                                 in ? a.cols - c : 0);
 #pragma unroll
@@ -393,6 +587,8 @@ __global__ void __launch_bounds__(64 * kGradWaves) k_adapter_grad(GradArgs a) {
 
 constexpr int64_t kMaxRows = 0x7FFFFFFF;
 
+bool misaligned(const void* p, int64_t bytes) { return (uintptr_t)p % (uintptr_t)bytes != 0; }
+
 int check_adapter(const nsc_adapter_desc* d) {
   NSC_REQUIRE_L(d != nullptr, NSC_E_INVAL, "adapter description is NULL");
   NSC_REQUIRE_L(d->k >= 1 && d->k <= (1 << 24) && d->d >= 1 && d->d <= (1 << 24), NSC_E_SHAPE,
@@ -411,10 +607,60 @@ int check_adapter(const nsc_adapter_desc* d) {
   return NSC_OK;
 }
 
-// Workspace: the rank-wide rows t (backward: and u), and backward the rows by
-// adapter.
+// How a product is split: tiles of tn outputs x tm rows and parts of the
+// reduction, chosen by the sizes alone.
+struct GemmPlan {
+  int32_t tn, tm, parts;
+};
+
+GemmPlan plan_gemm(int64_t max_rows, int64_t outs, int64_t len, int64_t es) {
+  GemmPlan p{};
+  // Large tiles read each operand least often; they need enough of them to
+  // fill the chip
+  auto tiles = [&](int64_t tn, int64_t tm) {
+    return (outs + tn - 1) / tn * ((max_rows + tm - 1) / tm);
+  };
+  p.tn = 128;
+  if (max_rows <= 16) p.tm = 16;
+  else if (tiles(128, 128) >= kNumCU) p.tm = 128;
+  else p.tm = 64;
+  const int64_t t = tiles(p.tn, p.tm), blocks = (len * es + 127) / 128;
+  // parts for about two workgroups per CU, each of at least four blocks
+  int64_t parts = t > 0 ? 2 * kNumCU / t : 1;
+  if (parts > blocks / 4) parts = blocks / 4;
+  if (parts > 64) parts = 64;
+  p.parts = parts < 1 ? 1 : (int32_t)parts;
+  return p;
+}
+
+size_t gemm_part_bytes(const GemmPlan& p, int64_t max_rows, int64_t outs) {
+  if (p.parts == 1) return 0;
+  return (size_t)((outs + p.tn - 1) / p.tn * p.tn) * ((max_rows + p.tm - 1) / p.tm * p.tm) *
+         p.parts * 4;
+}
+
+// Parts of the rank-wide rows' reduction: about four workgroups per CU, each
+// wave of at least two steps of 64 bytes.
+int32_t down_parts(int64_t max_rows, int64_t len, int64_t es) {
+  const int64_t tiles = (max_rows + 15) / 16;
+  int64_t parts = tiles > 0 ? 4 * kNumCU / tiles : 1;
+  const int64_t most = len * es / (64 * 2 * kDownWaves);
+  if (parts > most) parts = most;
+  if (parts > 8) parts = 8;
+  return parts < 1 ? 1 : (int32_t)parts;
+}
+
+// From this many rows on they are taken in the order of their adapters, so that
+// 16 neighbours mostly share one.
+constexpr int64_t kListRows = 256;
+
+// Workspace: the rank-wide rows t (backward: and u) by part, the product's
+// partial sums, and the rows by adapter.
 struct AdapterLayout {
-  size_t t, u, off, rows, total;
+  size_t t, u, part, off, rows, total;
+  int32_t t_parts, u_parts;
+  GemmPlan g;
+  bool list;
 };
 
 AdapterLayout adapter_layout(const nsc_adapter_desc& d, int64_t max_rows, bool backward) {
@@ -425,10 +671,16 @@ AdapterLayout adapter_layout(const nsc_adapter_desc& d, int64_t max_rows, bool b
     o = align_up(o + bytes, 256);
     return at;
   };
+  const int64_t es = type_bytes(d.dtype);
   const size_t rp = align_up(d.rank, 16);
-  L.t = take((size_t)max_rows * rp * 4);
-  if (backward) {
-    L.u = take((size_t)max_rows * rp * 4);
+  L.t_parts = down_parts(max_rows, d.k, es);
+  L.u_parts = down_parts(max_rows, d.d, es);
+  L.g = backward ? plan_gemm(max_rows, d.k, d.d, es) : plan_gemm(max_rows, d.d, d.k, es);
+  L.list = backward || max_rows >= kListRows;
+  L.t = take((size_t)max_rows * rp * 4 * L.t_parts);
+  if (backward) L.u = take((size_t)max_rows * rp * 4 * L.u_parts);
+  L.part = take(gemm_part_bytes(L.g, max_rows, backward ? d.k : d.d));
+  if (L.list) {
     L.off = take(((size_t)d.n_adapters + 1) * 4);
     L.rows = take((size_t)max_rows * 4);
   }
@@ -448,13 +700,11 @@ int check_adapter_call(const nsc_adapter_desc* d, int64_t max_rows, const void* 
   return NSC_OK;
 }
 
-bool misaligned(const void* p, int64_t bytes) { return (uintptr_t)p % (uintptr_t)bytes != 0; }
-
 template <typename T>
 int launch_down(const AdapterArgs& a, bool vec, bool b, hipStream_t st) {
   int64_t grid = (a.max_rows + 15) / 16;
   if (grid > 16 * kNumCU) grid = 16 * kNumCU;
-  const dim3 g((unsigned)grid), t(64 * kDownWaves);
+  const dim3 g((unsigned)grid, (unsigned)a.t_parts), t(64 * kDownWaves);
   if (b)
     hipLaunchKernelGGL((k_adapter_down<T, false, true>), g, t, 0, st, a);
   else if (vec)
@@ -465,23 +715,31 @@ int launch_down(const AdapterArgs& a, bool vec, bool b, hipStream_t st) {
   return NSC_OK;
 }
 
-template <typename T>
-int launch_gemm(const AdapterArgs& a, bool vec, bool tr, hipStream_t st) {
-  const int outs = tr ? a.k : a.d;
-  int64_t gy = (a.max_rows + kTile - 1) / kTile;
+template <typename T, bool VEC, bool TR, int TM>
+int launch_tiles(const AdapterArgs& a, hipStream_t st) {
+  constexpr int TN = 128;
+  using G = Gemm<T, TR, TN, TM>;
+  const int outs = TR ? a.k : a.d;
+  int64_t gy = (a.max_rows + TM - 1) / TM;
   if (gy > 65535) gy = 65535;
-  const dim3 g((unsigned)((outs + kTile - 1) / kTile), (unsigned)gy), t(256);
-#define NSC_GEMM(V, TR) hipLaunchKernelGGL((k_adapter_gemm<T, V, TR>), g, t, 0, st, a)
-  if (tr) {
-    if (vec) NSC_GEMM(true, true);
-    else NSC_GEMM(false, true);
-  } else {
-    if (vec) NSC_GEMM(true, false);
-    else NSC_GEMM(false, false);
-  }
-#undef NSC_GEMM
+  const dim3 g((unsigned)((outs + TN - 1) / TN), (unsigned)gy, (unsigned)a.parts), t(256);
+  hipLaunchKernelGGL((k_adapter_gemm<T, VEC, TR, TN, TM>), g, t, G::kLds, st, a);
   NSC_CHECK_LAUNCH("k_adapter_gemm");
+  if (a.parts > 1) {
+    hipLaunchKernelGGL((k_adapter_join<T, TR, TN, TM>), dim3(g.x, g.y), t, 0, st, a);
+    NSC_CHECK_LAUNCH("k_adapter_join");
+  }
   return NSC_OK;
+}
+
+template <typename T, bool TR>
+int launch_gemm(AdapterArgs a, const GemmPlan& p, bool vec, hipStream_t st) {
+  a.parts = p.parts;
+  if (p.tm == 128)
+    return vec ? launch_tiles<T, true, TR, 128>(a, st) : launch_tiles<T, false, TR, 128>(a, st);
+  if (p.tm == 64)
+    return vec ? launch_tiles<T, true, TR, 64>(a, st) : launch_tiles<T, false, TR, 64>(a, st);
+  return vec ? launch_tiles<T, true, TR, 16>(a, st) : launch_tiles<T, false, TR, 16>(a, st);
 }
 
 template <typename T>
@@ -492,6 +750,15 @@ int launch_grad(const GradArgs& a, bool b, hipStream_t st) {
   else
     hipLaunchKernelGGL((k_adapter_grad<T, false>), g, t, 0, st, a);
   NSC_CHECK_LAUNCH("k_adapter_grad");
+  return NSC_OK;
+}
+
+int launch_list(AdapterArgs* a, int32_t* off, int32_t* rows, hipStream_t st) {
+  const int32_t most = 8 * kNumCU;
+  hipLaunchKernelGGL(k_adapter_list, dim3((unsigned)(a->n_adapters < most ? a->n_adapters + 1 : most)),
+                     dim3(64 * kListWaves), 0, st, *a, off, rows);
+  NSC_CHECK_LAUNCH("k_adapter_list");
+  a->rows = rows;
   return NSC_OK;
 }
 
@@ -511,51 +778,79 @@ AdapterArgs adapter_args(const nsc_adapter_desc& d, const void* w, const void* a
   g.rank = d.rank;
   g.rp = (int32_t)align_up(d.rank, 16);
   g.n_adapters = d.n_adapters;
+  g.b4 = d.rank % 4 == 0 && !misaligned(b, 4 * type_bytes(d.dtype));
   return g;
 }
 
 template <typename T>
-int project(AdapterArgs a, bool vec, hipStream_t st) {
-  if (int rc = launch_down<T>(a, vec, false, st)) return rc;
-  return launch_gemm<T>(a, vec, false, st);
+int project(const nsc_adapter_desc& d, AdapterArgs a, unsigned char* ws, hipStream_t st) {
+  constexpr int E = 16 / sizeof(T);
+  const AdapterLayout L = adapter_layout(d, a.max_rows, false);
+  if (L.list)
+    if (int rc = launch_list(&a, reinterpret_cast<int32_t*>(ws + L.off),
+                             reinterpret_cast<int32_t*>(ws + L.rows), st))
+      return rc;
+  a.in_stride = d.x_stride;
+  a.out_stride = d.y_stride;
+  a.out4 = d.d % 4 == 0 && d.y_stride % 4 == 0 && !misaligned(a.out, 4 * sizeof(T));
+  a.t = reinterpret_cast<float*>(ws + L.t);
+  a.part = reinterpret_cast<float*>(ws + L.part);
+  a.t_parts = L.t_parts;
+  const bool rows16 = !misaligned(a.x, 16) && d.k % E == 0 && d.x_stride % E == 0;
+  if (int rc = launch_down<T>(a, rows16 && !misaligned(a.a, 16), false, st)) return rc;
+  return launch_gemm<T, false>(a, L.g, rows16 && !misaligned(a.w, 16), st);
 }
 
 template <typename T>
 int backward(const nsc_adapter_desc& d, AdapterArgs a, const void* x, const void* dy, void* dx,
-             float* da, float* db, float* t, float* u, int32_t* off, int32_t* rows, bool vec_x,
-             bool vec_dy, hipStream_t st) {
-  hipLaunchKernelGGL(k_adapter_list,
-                     dim3((unsigned)(d.n_adapters < 8 * kNumCU ? d.n_adapters : 8 * kNumCU)),
-                     dim3(64 * kListWaves), 0, st, a, off, rows);
-  NSC_CHECK_LAUNCH("k_adapter_list");
+             float* da, float* db, unsigned char* ws, hipStream_t st) {
+  constexpr int E = 16 / sizeof(T);
+  const AdapterLayout L = adapter_layout(d, a.max_rows, true);
+  float* t = reinterpret_cast<float*>(ws + L.t);
+  float* u = reinterpret_cast<float*>(ws + L.u);
+  int32_t* off = reinterpret_cast<int32_t*>(ws + L.off);
+  int32_t* rows = reinterpret_cast<int32_t*>(ws + L.rows);
+  if (int rc = launch_list(&a, off, rows, st)) return rc;
   if (a.max_rows > 0) {
     a.x = x;
     a.in_stride = d.x_stride;
     a.t = t;
-    if (int rc = launch_down<T>(a, vec_x, false, st)) return rc;
+    a.t_parts = L.t_parts;
+    if (int rc = launch_down<T>(
+            a, !misaligned(x, 16) && !misaligned(a.a, 16) && d.k % E == 0 && d.x_stride % E == 0,
+            false, st))
+      return rc;
     a.x = dy;
     a.in_stride = d.y_stride;
     a.t = u;
+    a.t_parts = L.u_parts;
     if (int rc = launch_down<T>(a, false, true, st)) return rc;
     if (dx) {
       a.out = dx;
       a.out_stride = d.x_stride;
-      if (int rc = launch_gemm<T>(a, vec_dy, true, st)) return rc;
+      a.out4 = d.k % 4 == 0 && d.x_stride % 4 == 0 && !misaligned(dx, 4 * sizeof(T));
+      a.part = reinterpret_cast<float*>(ws + L.part);
+      const bool vec = !misaligned(dy, 16) && !misaligned(a.w, 16) && d.d % E == 0 &&
+                       d.y_stride % E == 0 && d.k % E == 0;
+      if (int rc = launch_gemm<T, true>(a, L.g, vec, st)) return rc;
     }
   }
   GradArgs g{};
   g.off = off;
   g.rows = rows;
+  g.max_rows = a.max_rows;
   g.rank = a.rank;
   g.rp = a.rp;
   g.n_adapters = d.n_adapters;
   g.t = u;
+  g.t_parts = L.u_parts;
   g.v = x;
   g.v_stride = d.x_stride;
   g.cols = d.k;
   g.out = da;
   if (int rc = launch_grad<T>(g, false, st)) return rc;
   g.t = t;
+  g.t_parts = L.t_parts;
   g.v = dy;
   g.v_stride = d.y_stride;
   g.cols = d.d;
@@ -603,17 +898,12 @@ int nsc_adapter_project(const nsc_adapter_desc* desc, const void* x, const void*
   AdapterArgs g = adapter_args(*desc, w, a, b, scale, ids, count, max_rows);
   g.x = x;
   g.bias = bias;
-  g.in_stride = desc->x_stride;
   g.out = y;
-  g.out_stride = desc->y_stride;
-  g.t = static_cast<float*>(ws);
-  const int64_t e = 16 / es;
-  const bool vec = !misaligned(x, 16) && !misaligned(w, 16) && !misaligned(a, 16) &&
-                   desc->k % e == 0 && desc->x_stride % e == 0;
+  unsigned char* at = static_cast<unsigned char*>(ws);
   const hipStream_t st = (hipStream_t)stream;
-  if (desc->dtype == NSC_T_BF16) return project<__bf16>(g, vec, st);
-  if (desc->dtype == NSC_T_F16) return project<_Float16>(g, vec, st);
-  return project<float>(g, vec, st);
+  if (desc->dtype == NSC_T_BF16) return project<__bf16>(*desc, g, at, st);
+  if (desc->dtype == NSC_T_F16) return project<_Float16>(*desc, g, at, st);
+  return project<float>(*desc, g, at, st);
 }
 
 int nsc_adapter_backward(const nsc_adapter_desc* desc, const void* x, const void* dy,
@@ -633,22 +923,11 @@ int nsc_adapter_backward(const nsc_adapter_desc* desc, const void* x, const void
                 NSC_E_INVAL, "a pointer is not aligned to its elements");
   const AdapterArgs g =
       adapter_args(*desc, w, a, b, scale, ids, max_rows ? count : nullptr, max_rows);
-  const AdapterLayout L = adapter_layout(*desc, max_rows, true);
   unsigned char* at = static_cast<unsigned char*>(ws);
-  float* t = reinterpret_cast<float*>(at + L.t);
-  float* u = reinterpret_cast<float*>(at + L.u);
-  int32_t* off = reinterpret_cast<int32_t*>(at + L.off);
-  int32_t* rows = reinterpret_cast<int32_t*>(at + L.rows);
-  const int64_t e = 16 / es;
-  const bool vec_x = !misaligned(x, 16) && !misaligned(a, 16) && desc->k % e == 0 &&
-                     desc->x_stride % e == 0;
-  const bool vec_dy = !misaligned(dy, 16) && desc->d % e == 0 && desc->y_stride % e == 0;
   const hipStream_t st = (hipStream_t)stream;
-  if (desc->dtype == NSC_T_BF16)
-    return backward<__bf16>(*desc, g, x, dy, dx, da, db, t, u, off, rows, vec_x, vec_dy, st);
-  if (desc->dtype == NSC_T_F16)
-    return backward<_Float16>(*desc, g, x, dy, dx, da, db, t, u, off, rows, vec_x, vec_dy, st);
-  return backward<float>(*desc, g, x, dy, dx, da, db, t, u, off, rows, vec_x, vec_dy, st);
+  if (desc->dtype == NSC_T_BF16) return backward<__bf16>(*desc, g, x, dy, dx, da, db, at, st);
+  if (desc->dtype == NSC_T_F16) return backward<_Float16>(*desc, g, x, dy, dx, da, db, at, st);
+  return backward<float>(*desc, g, x, dy, dx, da, db, at, st);
 }
 
 }  // extern "C"
