@@ -15,6 +15,8 @@
 
 #include <limits.h>
 
+#include <type_traits>
+
 namespace nsc {
 namespace {
 
@@ -96,6 +98,9 @@ struct AdapterArgs {
   int32_t parts;            // parts of the product's reduction
   int32_t b4;               // four values of a row of b are one aligned load
   int32_t out4;             // four neighbouring outputs are one aligned store
+  int64_t row_tiles;        // the product's grid: out_tiles x row_tiles x parts, after
+  int32_t out_tiles;        // down_blocks workgroups of rank-wide rows
+  int32_t down_blocks;
 };
 
 __device__ __forceinline__ int64_t live_rows(const AdapterArgs& a) {
@@ -110,12 +115,15 @@ __device__ __forceinline__ int adapter_of(const AdapterArgs& a, int64_t row) {
   const int p = a.ids[row];
   return p >= 0 && p < a.n_adapters ? p : INT_MAX;
 }
-// The smallest adapter above p among 16 rows (INT_MAX: none).
-__device__ __forceinline__ int next_adapter(int mine, int p) {
-  int v = mine > p ? mine : INT_MAX;
-#pragma unroll
-  for (int o = 1; o < 16; o <<= 1) v = min(v, __shfl_xor(v, o, 64));
-  return __builtin_amdgcn_readfirstlane(v);
+// The lanes 0 .. 15 whose row has an adapter, and one of those rows' adapters.
+__device__ __forceinline__ uint32_t with_adapter(int mine) {
+  return (uint32_t)__ballot(mine != INT_MAX) & 0xFFFFu;
+}
+__device__ __forceinline__ int pick_adapter(int mine, uint32_t todo) {
+  return __builtin_amdgcn_readlane(mine, __builtin_ctz(todo));
+}
+__device__ __forceinline__ uint32_t rows_of(int mine, int p) {
+  return (uint32_t)__ballot(mine == p) & 0xFFFFu;
 }
 
 // Rank-wide rows of 16 positions: a workgroup per (tile, part of the
@@ -123,69 +131,100 @@ __device__ __forceinline__ int next_adapter(int mine, int p) {
 // lane keeps the products of its own row's adapter.  B = false: t = scale x a^T
 // over k; B = true: u = scale dy b over d, whose values lie rank apart.
 constexpr int kDownWaves = 4;
-constexpr int kDownUnroll = 4;  // steps whose loads are in flight together
+constexpr int kDownSteps = 4;  // steps whose loads are in flight together
 
 template <typename T, bool VEC, bool B>
-__global__ void __launch_bounds__(64 * kDownWaves) k_adapter_down(AdapterArgs a) {
+__device__ __forceinline__ void adapter_down(const AdapterArgs& a, int64_t block, int64_t blocks,
+                                             int part, f32x4 (*red)[64]) {
   using M = Mma<T>;
-  constexpr int KS = B ? 16 : M::KS;
-  __shared__ f32x4 red[kDownWaves][64];
+  constexpr int KS = B ? 16 : M::KS, S = kDownSteps;
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int m = lane & 15, g = lane >> 4;
   const int64_t n = live_rows(a);
   const int len = B ? a.d : a.k;
-  const int steps = (len + KS - 1) / KS, part = blockIdx.y * kDownWaves + wave;
-  const int s0 = (int)((int64_t)part * steps / (a.t_parts * kDownWaves));
-  const int s1 = (int)((int64_t)(part + 1) * steps / (a.t_parts * kDownWaves));
-  for (int64_t pos0 = blockIdx.x * 16ll; pos0 < n; pos0 += gridDim.x * 16ll) {
+  const int steps = (len + KS - 1) / KS, parts = a.t_parts * kDownWaves;
+  const int s0 = (int)((int64_t)(part * kDownWaves + wave) * steps / parts);
+  const int s1 = (int)((int64_t)(part * kDownWaves + wave + 1) * steps / parts);
+  for (int64_t pos0 = block * 16; pos0 < n; pos0 += blocks * 16) {
     const bool in = pos0 + m < n;
     const int64_t row = row_at(a, in ? pos0 + m : n - 1);
     const int mine = in ? adapter_of(a, row) : INT_MAX;
+    const float scale = mine != INT_MAX ? a.scale[mine] : 0.0f;
+    const uint32_t some = with_adapter(mine);
     const T* x = static_cast<const T*>(a.x) + row * a.in_stride;
     for (int j0 = 0; j0 < a.rp; j0 += 16) {
       f32x4 out = {0.f, 0.f, 0.f, 0.f};
       const int j = j0 + m;
-      for (int p = next_adapter(mine, -1); p != INT_MAX; p = next_adapter(mine, p)) {
-        f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-        if constexpr (B) {
-          const T* b = static_cast<const T*>(a.b) + (int64_t)p * a.d * a.rank + j;
-          for (int s = s0; s < s1; ++s) {
-            const int k = s * KS + 4 * g;
-            f32x4 bv;
+      if (some)
+        for (int s = s0; s < s1; s += S) {
+          typename std::conditional<B, f32x4, uint4>::type xv[S], wv[S];
+          auto inside = [&](int u) {  // values from step s + u's first of this lane on
+            return s + u < s1 ? len - (s + u) * KS - (B ? 4 : M::E) * g : 0;
+          };
+          auto load_w = [&](int p) {
+            if constexpr (B) {
+              const T* b = static_cast<const T*>(a.b) + (int64_t)p * a.d * a.rank + j;
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-              bv[e] = j < a.rank && k + e < len ? (float)b[(int64_t)(k + e) * a.rank] : 0.0f;
-            acc = mma_f32(bv, load4(x + k, len - k), acc);
-          }
-        } else {
-          const T* ar = static_cast<const T*>(a.a) + ((int64_t)p * a.rank + j) * a.k;
-          for (int s = s0; s < s1; s += kDownUnroll) {
-            uint4 av[kDownUnroll], xv[kDownUnroll];
+              for (int u = 0; u < S; ++u) {
+                const int k = (s + u) * KS + 4 * g, left = j < a.rank ? inside(u) : 0;
 #pragma unroll
-            for (int u = 0; u < kDownUnroll; ++u) {
-              const int k = (s + u) * KS + M::E * g;
-              const int left = s + u < s1 ? len - k : 0;
-              av[u] = load_frag<T, VEC>(ar + k, j < a.rank ? left : 0);
-              xv[u] = load_frag<T, VEC>(x + k, left);
+                for (int e = 0; e < 4; ++e)
+                  wv[u][e] = e < left ? (float)b[(int64_t)(k + e) * a.rank] : 0.0f;
+              }
+            } else {
+              const T* ar = static_cast<const T*>(a.a) + ((int64_t)p * a.rank + j) * a.k;
+#pragma unroll
+              for (int u = 0; u < S; ++u)
+                wv[u] = load_frag<T, VEC>(ar + (s + u) * KS + M::E * g, j < a.rank ? inside(u) : 0);
             }
+          };
+          uint32_t todo = some;
+          int p = pick_adapter(mine, todo);
+          load_w(p);
 #pragma unroll
-            for (int u = 0; u < kDownUnroll; ++u) acc = M::mma(av[u], xv[u], acc);
+          for (int u = 0; u < S; ++u) {
+            if constexpr (B)
+              xv[u] = load4(x + (s + u) * KS + 4 * g, inside(u));
+            else
+              xv[u] = load_frag<T, VEC>(x + (s + u) * KS + M::E * g, inside(u));
+          }
+          for (;;) {
+            f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int u = 0; u < S; ++u) {
+              if constexpr (B)
+                acc = mma_f32(wv[u], xv[u], acc);
+              else
+                acc = M::mma(wv[u], xv[u], acc);
+            }
+            const bool hit = mine == p;
+            todo &= ~rows_of(mine, p);
+            if (todo) {  // the next adapter's values while this one's products finish
+              p = pick_adapter(mine, todo);
+              load_w(p);
+            }
+            if (hit) out += acc;
+            if (!todo) break;
           }
         }
-        if (mine == p) out = acc * a.scale[p];
-      }
       __syncthreads();  // red is read before it is written again
       red[wave][lane] = out;
       __syncthreads();
       if (wave == 0 && in) {
 #pragma unroll
         for (int w = 1; w < kDownWaves; ++w) out += red[w][lane];
-        *reinterpret_cast<f32x4*>(a.t + ((int64_t)blockIdx.y * a.max_rows + pos0 + m) * a.rp + j0 +
-                                  4 * g) = out;
+        *reinterpret_cast<f32x4*>(a.t + (part * a.max_rows + pos0 + m) * a.rp + j0 + 4 * g) =
+            out * scale;
       }
     }
   }
+}
+
+template <typename T, bool VEC, bool B>
+__global__ void __launch_bounds__(64 * kDownWaves) k_adapter_down(AdapterArgs a) {
+  __shared__ f32x4 red[kDownWaves][64];
+  adapter_down<T, VEC, B>(a, blockIdx.x, gridDim.x, blockIdx.y, red);
 }
 
 // The shared product with the rank-wide rows' in its epilogue, in tiles of TN
@@ -253,58 +292,82 @@ __device__ __forceinline__ void copy_to_lds(const void* from, void* lds) {
                                    (__attribute__((address_space(3))) void*)lds, 16, 0, 0);
 }
 
+// Adds the rank-wide rows' products and the bias to outputs o0 .. of positions
+// pos0 .. and stores them.
 template <typename T, bool TR, int NI, int NJ>
 __device__ __forceinline__ void adapter_epilogue(const AdapterArgs& a, f32x4 (&acc)[NI][NJ],
                                                  int o0, int64_t pos0, int64_t n, int m, int g) {
   const int outs = TR ? a.k : a.d;
+  int64_t row[NJ];
+  int mine[NJ];
 #pragma unroll
-  for (int j = 0; j < NJ; ++j) {  // 16 positions
+  for (int j = 0; j < NJ; ++j) {
     const int64_t pos = pos0 + j * 16 + m;
-    const int64_t row = pos < n ? row_at(a, pos) : 0;
-    const int mine = pos < n ? adapter_of(a, row) : INT_MAX;
-    for (int p = next_adapter(mine, -1); p != INT_MAX; p = next_adapter(mine, p)) {
-      f32x4 add[NI];
+    row[j] = pos < n ? row_at(a, pos) : 0;
+    mine[j] = pos < n ? adapter_of(a, row[j]) : INT_MAX;
+  }
+  for (int q0 = 0; q0 < a.rp; q0 += 16) {
+    const int q = q0 + 4 * g;
+    f32x4 tv[NJ];
+    uint32_t todo[NJ];
 #pragma unroll
-      for (int i = 0; i < NI; ++i) add[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-      for (int q0 = 0; q0 < a.rp; q0 += 16) {
-        const int q = q0 + 4 * g;
-        f32x4 tv = {0.f, 0.f, 0.f, 0.f};
-        if (mine == p)
-          for (int h = 0; h < a.t_parts; ++h)
-            tv += *reinterpret_cast<const f32x4*>(a.t + (h * a.max_rows + pos) * a.rp + q);
+    for (int j = 0; j < NJ; ++j) {
+      tv[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+      todo[j] = with_adapter(mine[j]);
+      if (mine[j] != INT_MAX)
+        for (int h = 0; h < a.t_parts; ++h)
+          tv[j] += *reinterpret_cast<const f32x4*>(
+              a.t + (h * a.max_rows + pos0 + j * 16 + m) * a.rp + q);
+    }
+    for (;;) {
+      int p = INT_MAX;
 #pragma unroll
-        for (int i = 0; i < NI; ++i) {
-          const int o = o0 + i * 16 + m;
-          f32x4 bv = {0.f, 0.f, 0.f, 0.f};
-          if (o < outs) {
-            if constexpr (TR) {
-              const T* ap = static_cast<const T*>(a.a) + (int64_t)p * a.rank * a.k + o;
+      for (int j = 0; j < NJ; ++j)
+        if (p == INT_MAX && todo[j]) p = pick_adapter(mine[j], todo[j]);
+      if (p == INT_MAX) break;
+      f32x4 bv[NI];
 #pragma unroll
-              for (int e = 0; e < 4; ++e)
-                if (q + e < a.rank) bv[e] = (float)ap[(int64_t)(q + e) * a.k];
-            } else {
-              const T* bp = static_cast<const T*>(a.b) + ((int64_t)p * a.d + o) * a.rank + q;
-              if (a.b4) {
-                if (q < a.rank) {
-                  const Vec<T, 4> v = *reinterpret_cast<const Vec<T, 4>*>(bp);
+      for (int i = 0; i < NI; ++i) {
+        const int o = o0 + i * 16 + m;
+        bv[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+        if (o < outs) {
+          if constexpr (TR) {
+            const T* ap = static_cast<const T*>(a.a) + (int64_t)p * a.rank * a.k + o;
 #pragma unroll
-                  for (int e = 0; e < 4; ++e) bv[e] = (float)v.e[e];
-                }
-              } else {
-                bv = load4(bp, a.rank - q);
+            for (int e = 0; e < 4; ++e)
+              if (q + e < a.rank) bv[i][e] = (float)ap[(int64_t)(q + e) * a.k];
+          } else {
+            const T* bp = static_cast<const T*>(a.b) + ((int64_t)p * a.d + o) * a.rank + q;
+            if (a.b4) {
+              if (q < a.rank) {
+                const Vec<T, 4> v = *reinterpret_cast<const Vec<T, 4>*>(bp);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) bv[i][e] = (float)v.e[e];
               }
+            } else {
+              bv[i] = load4(bp, a.rank - q);
             }
           }
-          add[i] = mma_f32(bv, tv, add[i]);
         }
       }
-      if (mine == p) {
 #pragma unroll
-        for (int i = 0; i < NI; ++i) acc[i][j] += add[i];
+      for (int j = 0; j < NJ; ++j) {
+        const uint32_t hit = rows_of(mine[j], p);
+        if (hit) {
+          todo[j] &= ~hit;
+#pragma unroll
+          for (int i = 0; i < NI; ++i) {
+            const f32x4 add = mma_f32(bv[i], tv[j], f32x4{0.f, 0.f, 0.f, 0.f});
+            if (mine[j] == p) acc[i][j] += add;
+          }
+        }
       }
     }
-    if (pos < n) {
-      T* y = static_cast<T*>(a.out) + row * a.out_stride;
+  }
+#pragma unroll
+  for (int j = 0; j < NJ; ++j) {
+    if (pos0 + j * 16 + m < n) {
+      T* y = static_cast<T*>(a.out) + row[j] * a.out_stride;
 #pragma unroll
       for (int i = 0; i < NI; ++i) {
         const int o = o0 + i * 16 + 4 * g;
@@ -330,21 +393,34 @@ __global__ void __launch_bounds__(256) k_adapter_gemm(AdapterArgs a) {
   using M = Mma<T>;
   constexpr int E = G::E, BK = G::BK, NI = G::NI, NJ = G::NJ;
   extern __shared__ __align__(16) uint4 lds[];
+  int64_t block = blockIdx.x;
+  if constexpr (!TR) {  // a call whose product is split takes its rank-wide rows here
+    if (block < a.down_blocks) {
+      adapter_down<T, VEC, false>(a, block / a.t_parts, a.down_blocks / a.t_parts,
+                                  (int)(block % a.t_parts), reinterpret_cast<f32x4(*)[64]>(lds));
+      return;
+    }
+    block -= a.down_blocks;
+  }
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int m = lane & 15, g = lane >> 4;
   const int64_t n = live_rows(a);
   const int outs = TR ? a.k : a.d, len = TR ? a.d : a.k;
-  const int o0 = blockIdx.x * TN;
+  const int tx = (int)(block % a.out_tiles);
+  const int64_t ty = block / a.out_tiles % a.row_tiles;
+  const int z = (int)(block / a.out_tiles / a.row_tiles);
+  const int o0 = tx * TN;
   const int wo = (wave % G::WN) * NI * 16, wr = (wave / G::WN) * NJ * 16;
   const T* w = static_cast<const T*>(a.w);
   const T* xs = static_cast<const T*>(a.x);
   const int blocks = (len + BK - 1) / BK;
-  const int b0 = (int)((int64_t)blockIdx.z * blocks / a.parts);
-  const int b1 = (int)((int64_t)(blockIdx.z + 1) * blocks / a.parts);
+  const int b0 = (int)((int64_t)z * blocks / a.parts);
+  const int b1 = (int)((int64_t)(z + 1) * blocks / a.parts);
   constexpr int XC = (G::XCH + 255) / 256, WC = G::WCH / 256;  // chunks per thread
   static_assert(G::WCH % 256 == 0, "whole chunks per thread");
-  for (int64_t pos0 = blockIdx.y * (int64_t)TM; pos0 < n; pos0 += gridDim.y * (int64_t)TM) {
+  const int64_t pos0 = ty * TM;
+  if (pos0 < n) {
     f32x4 acc[NI][NJ];
 #pragma unroll
     for (int i = 0; i < NI; ++i)
@@ -426,11 +502,10 @@ __global__ void __launch_bounds__(256) k_adapter_gemm(AdapterArgs a) {
           for (int j = 0; j < NJ; ++j) acc[i][j] = M::mma(av[i], bv[j], acc[i][j]);
       }
     }
-    __syncthreads();  // the buffers are read before the next tile's copies
     if (a.parts > 1) {
-      const int64_t tile = (pos0 / TM) * gridDim.x + blockIdx.x;
       f32x4* out = reinterpret_cast<f32x4*>(a.part) +
-                   (tile * a.parts + blockIdx.z) * (TN * TM / 4) + wave * NI * NJ * 64 + lane;
+                   ((ty * a.out_tiles + tx) * a.parts + z) * (TN * TM / 4) + wave * NI * NJ * 64 +
+                   lane;
 #pragma unroll
       for (int i = 0; i < NI; ++i)
 #pragma unroll
@@ -441,33 +516,26 @@ __global__ void __launch_bounds__(256) k_adapter_gemm(AdapterArgs a) {
   }
 }
 
-// Adds a tile's parts in order, then its epilogue: a workgroup per tile.
+// Adds a tile's parts in order, then its epilogue: a wave per 16 outputs of 16
+// rows.
 template <typename T, bool TR, int TN, int TM>
 __global__ void __launch_bounds__(256) k_adapter_join(AdapterArgs a) {
   using G = Gemm<T, TR, TN, TM>;
-  constexpr int NI = G::NI, NJ = G::NJ;
+  constexpr int NI = G::NI, NJ = G::NJ, F = TN * TM / 256;  // 16 x 16 blocks of a tile
   const int lane = threadIdx.x & 63;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t item = blockIdx.x * 4ll + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t tile = item / F;
+  const int f = (int)(item % F), wave = f / (NI * NJ), i = f % (NI * NJ) / NJ, j = f % NJ;
   const int64_t n = live_rows(a);
-  for (int64_t pos0 = blockIdx.y * (int64_t)TM; pos0 < n; pos0 += gridDim.y * (int64_t)TM) {
-    const int64_t tile = (pos0 / TM) * gridDim.x + blockIdx.x;
-    const f32x4* in = reinterpret_cast<const f32x4*>(a.part) + tile * a.parts * (TN * TM / 4) +
-                      wave * NI * NJ * 64 + lane;
-    f32x4 acc[NI][NJ];
-#pragma unroll
-    for (int i = 0; i < NI; ++i)
-#pragma unroll
-      for (int j = 0; j < NJ; ++j) acc[i][j] = in[(i * NJ + j) * 64];
-    for (int h = 1; h < a.parts; ++h) {
-      in += TN * TM / 4;
-#pragma unroll
-      for (int i = 0; i < NI; ++i)
-#pragma unroll
-        for (int j = 0; j < NJ; ++j) acc[i][j] += in[(i * NJ + j) * 64];
-    }
-    adapter_epilogue<T, TR, NI, NJ>(a, acc, blockIdx.x * TN + (wave % G::WN) * NI * 16,
-                                    pos0 + (wave / G::WN) * NJ * 16, n, lane & 15, lane >> 4);
-  }
+  const int64_t pos0 = tile / a.out_tiles * TM + (wave / G::WN) * NJ * 16 + j * 16;
+  const int o0 = (int)(tile % a.out_tiles) * TN + (wave % G::WN) * NI * 16 + i * 16;
+  if (pos0 >= n || o0 >= (TR ? a.k : a.d)) return;
+  const f32x4* in =
+      reinterpret_cast<const f32x4*>(a.part) + tile * a.parts * (TN * TM / 4) + f * 64 + lane;
+  f32x4 acc[1][1] = {{in[0]}};
+#pragma unroll 8
+  for (int h = 1; h < a.parts; ++h) acc[0][0] += in[(int64_t)h * (TN * TM / 4)];
+  adapter_epilogue<T, TR, 1, 1>(a, acc, o0, pos0, n, lane & 15, lane >> 4);
 }
 
 // The rows of each adapter in ascending order: rows[off[p] .. off[p + 1]), and
@@ -513,72 +581,89 @@ __global__ void __launch_bounds__(64 * kListWaves) k_adapter_list(AdapterArgs a,
   }
 }
 
-// A gradient of the adapters: a workgroup takes 64 columns of the rows of one
-// adapter, its waves every eighth step of 16 rows, 16 of the rank at a time.
-// B = false: da[p][j][c] = sum u[r][j] x[r][c]; B = true: db[p][c][j] = sum
-// t[r][j] dy[r][c].
-constexpr int kGradWaves = 8;
-
+// The gradients of the adapters: a wave takes the 16 rank values j0 .. of one
+// adapter and 16 x CPL columns, a lane CPL neighbouring ones (16 bytes of a
+// row), and adds u^T x (or t^T dy) over the adapter's rows, 16 at a time.  RW
+// waves share them and add their sums through LDS; the other waves of a
+// workgroup take other columns.
 struct GradArgs {
-  const float* t;           // u, or t: [t_parts][max_rows][rp]
-  const void* v;            // x, or dy
-  int64_t v_stride;
+  const float* t[2];        // u, t: [parts][max_rows][rp]
+  const void* v[2];         // x, dy
+  float* out[2];            // da, db
+  int64_t v_stride[2];
+  int32_t parts[2], cols[2];
+  int32_t vec[2];           // a lane's columns are one aligned load
+  int32_t blocks0;          // workgroups per adapter that take da's columns
   const int32_t* off;
   const int32_t* rows;
-  float* out;
   int64_t max_rows;
-  int32_t cols, rank, rp, n_adapters, t_parts;
+  int32_t rank, rp;
 };
 
-template <typename T, bool B>
-__global__ void __launch_bounds__(64 * kGradWaves) k_adapter_grad(GradArgs a) {
-  __shared__ f32x4 red[kGradWaves][4][64];
+template <typename T, int RW>
+__global__ void __launch_bounds__(512) k_adapter_grad(GradArgs a) {
+  constexpr int CPL = 16 / sizeof(T), CW = 8 / RW;  // waves along the columns
+  __shared__ f32x4 red[RW > 1 ? 8 : 1][CPL][RW > 1 ? 64 : 1];
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int m = lane & 15, g = lane >> 4;
-  const int c0 = blockIdx.x * 64, c = c0 + 4 * m;  // a lane's four columns
-  for (int p = blockIdx.y; p < a.n_adapters; p += gridDim.y) {
-    const int32_t b = a.off[p], e = a.off[p + 1];
-    for (int j0 = 0; j0 < a.rp; j0 += 16) {
-      f32x4 acc[4];
+  const int m = lane & 15, g = lane >> 4, rw = wave % RW;
+  const int which = (int)blockIdx.x >= a.blocks0, p = blockIdx.y;
+  const int blk = (int)blockIdx.x - (which ? a.blocks0 : 0);
+  const int cols = which ? a.cols[1] : a.cols[0], parts = which ? a.parts[1] : a.parts[0];
+  const bool vec = (which ? a.vec[1] : a.vec[0]) != 0;
+  const int64_t stride = which ? a.v_stride[1] : a.v_stride[0];
+  const float* t = which ? a.t[1] : a.t[0];
+  const T* v = static_cast<const T*>(which ? a.v[1] : a.v[0]);
+  float* out = which ? a.out[1] : a.out[0];
+  const int c = (blk * CW + wave / RW) * 16 * CPL + m * CPL;
+  const int32_t b = a.off[p], e = a.off[p + 1];
+  for (int j0 = 0; j0 < a.rp; j0 += 16) {
+    f32x4 acc[CPL];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) acc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-      for (int32_t r = b + wave * 16; r < e; r += 16 * kGradWaves) {
-        f32x4 uv, xv[4];
+    for (int i = 0; i < CPL; ++i) acc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int32_t r = b + rw * 16; r < e; r += 16 * RW) {
+      f32x4 uv;
+      uint4 xv[4];
 #pragma unroll
-        for (int s = 0; s < 4; ++s) {
-          const int32_t at = r + 4 * g + s;
-          const bool in = at < e;
-          const int64_t row = in ? a.rows[at] : 0;
-          uv[s] = 0.0f;
-          for (int h = 0; in && h < a.t_parts; ++h)
-            uv[s] += a.t[(h * a.max_rows + at) * a.rp + j0 + m];
-          const f32x4 v = load4(static_cast<const T*>(a.v) + row * a.v_stride + c,
-                                in ? a.cols - c : 0);
-#pragma unroll
-          for (int i = 0; i < 4; ++i) xv[i][s] = v[i];
-        }
-#pragma unroll
-        for (int i = 0; i < 4; ++i) acc[i] = mma_f32(uv, xv[i], acc[i]);
+      for (int s = 0; s < 4; ++s) {
+        const int32_t at = r + 4 * g + s;
+        const bool in = at < e;
+        const T* x = v + (in ? a.rows[at] : 0) * stride + c;
+        xv[s] = vec ? load_frag<T, true>(x, in ? cols - c : 0)
+                    : load_frag<T, false>(x, in ? cols - c : 0);
+        uv[s] = 0.0f;
+        for (int h = 0; in && h < parts; ++h) uv[s] += t[(h * a.max_rows + at) * a.rp + j0 + m];
       }
-      __syncthreads();
 #pragma unroll
-      for (int i = 0; i < 4; ++i) red[wave][i][lane] = acc[i];
-      __syncthreads();
-      // wave i adds column i of the lanes' four: rank values j0 + 4 g .. + 3
-      if (wave < 4 && c + wave < a.cols) {
-        f32x4 s = red[0][wave][lane];
+      for (int i = 0; i < CPL; ++i) {
+        f32x4 xi;
 #pragma unroll
-        for (int w = 1; w < kGradWaves; ++w) s += red[w][wave][lane];
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          const int j = j0 + 4 * g + q;
-          if (j < a.rank)
-            a.out[B ? ((int64_t)p * a.cols + c + wave) * a.rank + j
-                    : ((int64_t)p * a.rank + j) * a.cols + c + wave] = s[q];
-        }
+        for (int s = 0; s < 4; ++s) xi[s] = (float)__builtin_bit_cast(Vec<T, CPL>, xv[s]).e[i];
+        acc[i] = mma_f32(uv, xi, acc[i]);
       }
+    }
+    if constexpr (RW > 1) {
+      __syncthreads();  // red is read before it is written again
+#pragma unroll
+      for (int i = 0; i < CPL; ++i) red[wave][i][lane] = acc[i];
       __syncthreads();
+      if (rw == 0) {
+#pragma unroll
+        for (int i = 0; i < CPL; ++i)
+#pragma unroll
+          for (int w = 1; w < RW; ++w) acc[i] += red[wave + w][i][lane];
+      }
+    }
+    if (rw == 0) {
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const int j = j0 + 4 * g + q;
+#pragma unroll
+        for (int i = 0; i < CPL; ++i)
+          if (j < a.rank && c + i < cols)
+            out[which ? ((int64_t)p * cols + c + i) * a.rank + j
+                      : ((int64_t)p * a.rank + j) * cols + c + i] = acc[i][q];
+      }
     }
   }
 }
@@ -622,11 +707,11 @@ GemmPlan plan_gemm(int64_t max_rows, int64_t outs, int64_t len, int64_t es) {
   };
   p.tn = 128;
   if (max_rows <= 16) p.tm = 16;
-  else if (tiles(128, 128) >= kNumCU) p.tm = 128;
+  else if (tiles(128, 128) >= 2 * kNumCU) p.tm = 128;
   else p.tm = 64;
   const int64_t t = tiles(p.tn, p.tm), blocks = (len * es + 127) / 128;
   // parts for about two workgroups per CU, each of at least four blocks
-  int64_t parts = t > 0 ? 2 * kNumCU / t : 1;
+  int64_t parts = t > 0 && t < kNumCU ? 2 * kNumCU / t : 1;
   if (parts > blocks / 4) parts = blocks / 4;
   if (parts > 64) parts = 64;
   p.parts = parts < 1 ? 1 : (int32_t)parts;
@@ -716,25 +801,28 @@ int launch_down(const AdapterArgs& a, bool vec, bool b, hipStream_t st) {
 }
 
 template <typename T, bool VEC, bool TR, int TM>
-int launch_tiles(const AdapterArgs& a, hipStream_t st) {
+int launch_tiles(AdapterArgs a, hipStream_t st) {
   constexpr int TN = 128;
   using G = Gemm<T, TR, TN, TM>;
-  const int outs = TR ? a.k : a.d;
-  int64_t gy = (a.max_rows + TM - 1) / TM;
-  if (gy > 65535) gy = 65535;
-  const dim3 g((unsigned)((outs + TN - 1) / TN), (unsigned)gy, (unsigned)a.parts), t(256);
-  hipLaunchKernelGGL((k_adapter_gemm<T, VEC, TR, TN, TM>), g, t, G::kLds, st, a);
+  a.out_tiles = ((TR ? a.k : a.d) + TN - 1) / TN;
+  a.row_tiles = (a.max_rows + TM - 1) / TM;
+  const int64_t tiles = a.out_tiles * a.row_tiles, grid = tiles * a.parts + a.down_blocks;
+  if (grid > 0x7FFFFFFF)
+    return fail(NSC_E_SHAPE, "%lld rows onto %d outputs are more tiles than a launch holds",
+                (long long)a.max_rows, TR ? a.k : a.d);
+  hipLaunchKernelGGL((k_adapter_gemm<T, VEC, TR, TN, TM>), dim3((unsigned)grid), dim3(256),
+                     G::kLds, st, a);
   NSC_CHECK_LAUNCH("k_adapter_gemm");
   if (a.parts > 1) {
-    hipLaunchKernelGGL((k_adapter_join<T, TR, TN, TM>), dim3(g.x, g.y), t, 0, st, a);
+    hipLaunchKernelGGL((k_adapter_join<T, TR, TN, TM>), dim3((unsigned)(tiles * (TN * TM / 1024))),
+                       dim3(256), 0, st, a);
     NSC_CHECK_LAUNCH("k_adapter_join");
   }
   return NSC_OK;
 }
 
 template <typename T, bool TR>
-int launch_gemm(AdapterArgs a, const GemmPlan& p, bool vec, hipStream_t st) {
-  a.parts = p.parts;
+int launch_gemm(const AdapterArgs& a, const GemmPlan& p, bool vec, hipStream_t st) {
   if (p.tm == 128)
     return vec ? launch_tiles<T, true, TR, 128>(a, st) : launch_tiles<T, false, TR, 128>(a, st);
   if (p.tm == 64)
@@ -742,13 +830,20 @@ int launch_gemm(AdapterArgs a, const GemmPlan& p, bool vec, hipStream_t st) {
   return vec ? launch_tiles<T, true, TR, 16>(a, st) : launch_tiles<T, false, TR, 16>(a, st);
 }
 
+// Eight waves share an adapter's rows where there are many of them on average,
+// else each takes columns of its own.
 template <typename T>
-int launch_grad(const GradArgs& a, bool b, hipStream_t st) {
-  const dim3 g((unsigned)((a.cols + 63) / 64), (unsigned)a.n_adapters), t(64 * kGradWaves);
-  if (b)
-    hipLaunchKernelGGL((k_adapter_grad<T, true>), g, t, 0, st, a);
+int launch_grad(GradArgs a, int32_t n_adapters, hipStream_t st) {
+  constexpr int CPL = 16 / sizeof(T);
+  const bool share = a.max_rows / n_adapters >= 512;
+  const int32_t width = 16 * CPL * (share ? 1 : 8);
+  a.blocks0 = (a.cols[0] + width - 1) / width;
+  const dim3 g((unsigned)(a.blocks0 + (a.cols[1] + width - 1) / width), (unsigned)n_adapters),
+      t(512);
+  if (share)
+    hipLaunchKernelGGL((k_adapter_grad<T, 8>), g, t, 0, st, a);
   else
-    hipLaunchKernelGGL((k_adapter_grad<T, false>), g, t, 0, st, a);
+    hipLaunchKernelGGL((k_adapter_grad<T, 1>), g, t, 0, st, a);
   NSC_CHECK_LAUNCH("k_adapter_grad");
   return NSC_OK;
 }
@@ -796,9 +891,15 @@ int project(const nsc_adapter_desc& d, AdapterArgs a, unsigned char* ws, hipStre
   a.t = reinterpret_cast<float*>(ws + L.t);
   a.part = reinterpret_cast<float*>(ws + L.part);
   a.t_parts = L.t_parts;
-  const bool rows16 = !misaligned(a.x, 16) && d.k % E == 0 && d.x_stride % E == 0;
-  if (int rc = launch_down<T>(a, rows16 && !misaligned(a.a, 16), false, st)) return rc;
-  return launch_gemm<T, false>(a, L.g, rows16 && !misaligned(a.w, 16), st);
+  a.parts = L.g.parts;
+  const bool vec = !misaligned(a.x, 16) && !misaligned(a.a, 16) && !misaligned(a.w, 16) &&
+                   d.k % E == 0 && d.x_stride % E == 0;
+  if (a.parts > 1) {
+    a.down_blocks = (int32_t)((a.max_rows + 15) / 16) * a.t_parts;
+  } else if (int rc = launch_down<T>(a, vec, false, st)) {
+    return rc;
+  }
+  return launch_gemm<T, false>(a, L.g, vec, st);
 }
 
 template <typename T>
@@ -830,6 +931,7 @@ int backward(const nsc_adapter_desc& d, AdapterArgs a, const void* x, const void
       a.out_stride = d.x_stride;
       a.out4 = d.k % 4 == 0 && d.x_stride % 4 == 0 && !misaligned(dx, 4 * sizeof(T));
       a.part = reinterpret_cast<float*>(ws + L.part);
+      a.parts = L.g.parts;
       const bool vec = !misaligned(dy, 16) && !misaligned(a.w, 16) && d.d % E == 0 &&
                        d.y_stride % E == 0 && d.k % E == 0;
       if (int rc = launch_gemm<T, true>(a, L.g, vec, st)) return rc;
@@ -841,21 +943,19 @@ int backward(const nsc_adapter_desc& d, AdapterArgs a, const void* x, const void
   g.max_rows = a.max_rows;
   g.rank = a.rank;
   g.rp = a.rp;
-  g.n_adapters = d.n_adapters;
-  g.t = u;
-  g.t_parts = L.u_parts;
-  g.v = x;
-  g.v_stride = d.x_stride;
-  g.cols = d.k;
-  g.out = da;
-  if (int rc = launch_grad<T>(g, false, st)) return rc;
-  g.t = t;
-  g.t_parts = L.t_parts;
-  g.v = dy;
-  g.v_stride = d.y_stride;
-  g.cols = d.d;
-  g.out = db;
-  return launch_grad<T>(g, true, st);
+  const void* v[2] = {x, dy};
+  const int64_t strides[2] = {d.x_stride, d.y_stride};
+  const int32_t cols[2] = {d.k, d.d};
+  for (int i = 0; i < 2; ++i) {
+    g.t[i] = i ? t : u;
+    g.parts[i] = i ? L.t_parts : L.u_parts;
+    g.v[i] = v[i];
+    g.v_stride[i] = strides[i];
+    g.cols[i] = cols[i];
+    g.vec[i] = !misaligned(v[i], 16) && strides[i] % E == 0 && cols[i] % E == 0;
+    g.out[i] = i ? db : da;
+  }
+  return launch_grad<T>(g, d.n_adapters, st);
 }
 
 }  // namespace
