@@ -130,10 +130,9 @@ __device__ __forceinline__ uint32_t rows_of(int mine, int p) {
 // reduction), whose waves split the part and add their sums through LDS.  A
 // lane keeps the products of its own row's adapter.  B = false: t = scale x a^T
 // over k; B = true: u = scale dy b over d, whose values lie rank apart.
-constexpr int kDownWaves = 4;
 constexpr int kDownSteps = 4;  // steps whose loads are in flight together
 
-template <typename T, bool VEC, bool B>
+template <typename T, bool VEC, bool B, int W>
 __device__ __forceinline__ void adapter_down(const AdapterArgs& a, int64_t block, int64_t blocks,
                                              int part, f32x4 (*red)[64]) {
   using M = Mma<T>;
@@ -143,9 +142,9 @@ __device__ __forceinline__ void adapter_down(const AdapterArgs& a, int64_t block
   const int m = lane & 15, g = lane >> 4;
   const int64_t n = live_rows(a);
   const int len = B ? a.d : a.k;
-  const int steps = (len + KS - 1) / KS, parts = a.t_parts * kDownWaves;
-  const int s0 = (int)((int64_t)(part * kDownWaves + wave) * steps / parts);
-  const int s1 = (int)((int64_t)(part * kDownWaves + wave + 1) * steps / parts);
+  const int steps = (len + KS - 1) / KS, parts = a.t_parts * W;
+  const int s0 = (int)((int64_t)(part * W + wave) * steps / parts);
+  const int s1 = (int)((int64_t)(part * W + wave + 1) * steps / parts);
   for (int64_t pos0 = block * 16; pos0 < n; pos0 += blocks * 16) {
     const bool in = pos0 + m < n;
     const int64_t row = row_at(a, in ? pos0 + m : n - 1);
@@ -213,7 +212,7 @@ __device__ __forceinline__ void adapter_down(const AdapterArgs& a, int64_t block
       __syncthreads();
       if (wave == 0 && in) {
 #pragma unroll
-        for (int w = 1; w < kDownWaves; ++w) out += red[w][lane];
+        for (int w = 1; w < W; ++w) out += red[w][lane];
         *reinterpret_cast<f32x4*>(a.t + (part * a.max_rows + pos0 + m) * a.rp + j0 + 4 * g) =
             out * scale;
       }
@@ -221,17 +220,23 @@ __device__ __forceinline__ void adapter_down(const AdapterArgs& a, int64_t block
   }
 }
 
+constexpr int kDownWaves = 16;  // alone in a launch; kGemmDownWaves beside the product
+constexpr int kGemmDownWaves = 4;
+constexpr int kMaxDownParts = 8;
+
 template <typename T, bool VEC, bool B>
 __global__ void __launch_bounds__(64 * kDownWaves) k_adapter_down(AdapterArgs a) {
   __shared__ f32x4 red[kDownWaves][64];
-  adapter_down<T, VEC, B>(a, blockIdx.x, gridDim.x, blockIdx.y, red);
+  adapter_down<T, VEC, B, kDownWaves>(a, blockIdx.x, gridDim.x, 0, red);
 }
 
 // The shared product with the rank-wide rows' in its epilogue, in tiles of TN
 // outputs x TM rows.  The reduction goes through LDS 128 bytes of a row at a
-// time, copied there directly from memory while the previous 128 are
-// multiplied; what lies behind the reduction's end, or is not aligned to 16
-// bytes, is loaded through registers and filled with zeros.
+// time, copied there directly from memory: STAGES blocks lie in LDS, one being
+// multiplied while the copies of the others are under way (with one block
+// ahead, its copies' latency of about 2 us was longer than the products of a
+// block).  What lies behind the reduction's end, or is not aligned to 16 bytes,
+// is loaded through registers and filled with zeros.
 // TR = false: outputs d from x w^T + t b^T.  TR = true: outputs k from
 // dy w + u a; the weights' reduction then runs down the columns of w, whose
 // tile keeps its rows in LDS and is transposed as it is read.
@@ -241,12 +246,15 @@ template <typename T, bool TR, int TN, int TM>
 struct Gemm {
   using M = Mma<T>;
   static constexpr int E = M::E, BK = 2 * M::KS;      // values per 16 and per 128 bytes
+  static constexpr int kWaves = TN >= 256 ? 8 : 4, kThreads = 64 * kWaves;
   static constexpr int WM = TM >= 64 ? 2 : 1;         // waves along the rows
-  static constexpr int WN = 4 / WM;                   // and along the outputs
+  static constexpr int WN = kWaves / WM;              // and along the outputs
   static constexpr int NI = TN / WN / 16, NJ = TM / WM / 16;
   static constexpr int WCH = TN * BK * sizeof(T) / 16, XCH = TM * 8;  // 16-byte chunks of a tile
   static constexpr int RCH = TR ? TN / E : 8;         // chunks of a row of the weights' tile
-  static constexpr size_t kLds = 2 * (WCH + XCH) * 16;
+  static constexpr int kStages = TM >= 64 ? 3 : 4;
+  // copies per thread and block, at least (a wave's outstanding ones of a whole block)
+  static constexpr int kCopies = WCH / kThreads + XCH / kThreads;
 
   // Chunk c of row r lies at chunk slot(r, c) of its row, so that the lanes of
   // a read fall on different banks: x and w by rows (16 lanes read one chunk
@@ -293,8 +301,8 @@ __device__ __forceinline__ void copy_to_lds(const void* from, void* lds) {
 }
 
 // Adds the rank-wide rows' products and the bias to outputs o0 .. of positions
-// pos0 .. and stores them.
-template <typename T, bool TR, int NI, int NJ>
+// pos0 .. and stores them.  TP: most parts of the rank-wide rows.
+template <typename T, bool TR, int NI, int NJ, int TP>
 __device__ __forceinline__ void adapter_epilogue(const AdapterArgs& a, f32x4 (&acc)[NI][NJ],
                                                  int o0, int64_t pos0, int64_t n, int m, int g) {
   const int outs = TR ? a.k : a.d;
@@ -314,10 +322,18 @@ __device__ __forceinline__ void adapter_epilogue(const AdapterArgs& a, f32x4 (&a
     for (int j = 0; j < NJ; ++j) {
       tv[j] = f32x4{0.f, 0.f, 0.f, 0.f};
       todo[j] = with_adapter(mine[j]);
-      if (mine[j] != INT_MAX)
-        for (int h = 0; h < a.t_parts; ++h)
-          tv[j] += *reinterpret_cast<const f32x4*>(
-              a.t + (h * a.max_rows + pos0 + j * 16 + m) * a.rp + q);
+      if (mine[j] != INT_MAX) {
+        f32x4 v[TP];
+#pragma unroll
+        for (int h = 0; h < TP; ++h) {
+          v[h] = f32x4{0.f, 0.f, 0.f, 0.f};
+          if (h == 0 || h < a.t_parts)
+            v[h] = *reinterpret_cast<const f32x4*>(
+                a.t + (h * a.max_rows + pos0 + j * 16 + m) * a.rp + q);
+        }
+#pragma unroll
+        for (int h = 0; h < TP; ++h) tv[j] += v[h];
+      }
     }
     for (;;) {
       int p = INT_MAX;
@@ -352,20 +368,28 @@ __device__ __forceinline__ void adapter_epilogue(const AdapterArgs& a, f32x4 (&a
       }
 #pragma unroll
       for (int j = 0; j < NJ; ++j) {
+        __builtin_amdgcn_sched_barrier(0);
         const uint32_t hit = rows_of(mine[j], p);
         if (hit) {
           todo[j] &= ~hit;
 #pragma unroll
           for (int i = 0; i < NI; ++i) {
             const f32x4 add = mma_f32(bv[i], tv[j], f32x4{0.f, 0.f, 0.f, 0.f});
-            if (mine[j] == p) acc[i][j] += add;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc[i][j][e] += mine[j] == p ? add[e] : 0.0f;
           }
         }
       }
     }
   }
+  f32x4 bias[NI];
+#pragma unroll
+  for (int i = 0; i < NI; ++i)
+    bias[i] = a.bias ? load4(a.bias + o0 + i * 16 + 4 * g, outs - o0 - i * 16 - 4 * g)
+                     : f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
   for (int j = 0; j < NJ; ++j) {
+    __builtin_amdgcn_sched_barrier(0);  // one row at a time: registers
     if (pos0 + j * 16 + m < n) {
       T* y = static_cast<T*>(a.out) + row[j] * a.out_stride;
 #pragma unroll
@@ -373,8 +397,7 @@ __device__ __forceinline__ void adapter_epilogue(const AdapterArgs& a, f32x4 (&a
         const int o = o0 + i * 16 + 4 * g;
         Vec<T, 4> v;
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-          v.e[e] = (T)(acc[i][j][e] + (a.bias && o + e < outs ? a.bias[o + e] : 0.0f));
+        for (int e = 0; e < 4; ++e) v.e[e] = (T)(acc[i][j][e] + bias[i][e]);
         if (a.out4) {
           if (o < outs) *reinterpret_cast<Vec<T, 4>*>(y + o) = v;
         } else {
@@ -387,17 +410,64 @@ __device__ __forceinline__ void adapter_epilogue(const AdapterArgs& a, f32x4 (&a
   }
 }
 
+// Waits until at most N of the wave's copies are under way and its LDS writes
+// have landed, then for the workgroup's other waves.
+template <int N>
+__device__ __forceinline__ void wait_copies() {
+  asm volatile("" ::: "memory");
+  // vmcnt(N) lgkmcnt(0); the builtin's wait is one the compiler counts with
+  __builtin_amdgcn_s_waitcnt((N & 15) | (N >> 4) << 14 | 0x70);
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+
+// A block's products from its tiles.
+template <typename G, typename M, int NI, int NJ>
+__device__ __forceinline__ void multiply(const uint4* wl, const uint4* xl, f32x4 (&acc)[NI][NJ],
+                                         int wo, int wr, int m, int g) {
+#pragma unroll
+  for (int s = 0; s < 2; ++s) {
+    uint4 av[NI], bv[NJ];
+#pragma unroll
+    for (int i = 0; i < NI; ++i) av[i] = G::wfrag(wl, wo + i * 16, s, m, g);
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) {
+      const int r = wr + j * 16 + m;
+      bv[j] = xl[r * 8 + G::xslot(r, 4 * s + g)];
+    }
+#pragma unroll
+    for (int i = 0; i < NI; ++i)
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) acc[i][j] = M::mma(av[i], bv[j], acc[i][j]);
+  }
+}
+
+// Tile of a logical index: panels of four tiles of outputs, row tile by row
+// tile, so that neighbours share both operands in a cache.
+__device__ __forceinline__ void tile_at(const AdapterArgs& a, int64_t i, int& tx, int64_t& ty) {
+  const int64_t panel = i / (4 * a.row_tiles);
+  const int width = min(4, a.out_tiles - (int)panel * 4);
+  i -= panel * 4 * a.row_tiles;
+  ty = i / width;
+  tx = (int)(panel * 4 + i % width);
+}
+
 template <typename T, bool VEC, bool TR, int TN, int TM>
-__global__ void __launch_bounds__(256) k_adapter_gemm(AdapterArgs a) {
+__global__ void __launch_bounds__(TN >= 256 ? 512 : 256) k_adapter_gemm(AdapterArgs a) {
   using G = Gemm<T, TR, TN, TM>;
   using M = Mma<T>;
-  constexpr int E = G::E, BK = G::BK, NI = G::NI, NJ = G::NJ;
-  extern __shared__ __align__(16) uint4 lds[];
+  constexpr int E = G::E, BK = G::BK, NI = G::NI, NJ = G::NJ, TH = G::kThreads, ST = G::kStages;
+  // A variable per stage, each named where it is used: of one array, the
+  // compiler takes every read to need all the copies under way and waits for
+  // them before it.
+  constexpr int kStage = G::WCH + G::XCH;
+  __shared__ uint4 stage0[kStage], stage1[kStage], stage2[kStage], stage3[ST > 3 ? kStage : 1];
   int64_t block = blockIdx.x;
-  if constexpr (!TR) {  // a call whose product is split takes its rank-wide rows here
+  if constexpr (!TR && TN < 256) {  // a call whose product is split takes its rank-wide rows here
     if (block < a.down_blocks) {
-      adapter_down<T, VEC, false>(a, block / a.t_parts, a.down_blocks / a.t_parts,
-                                  (int)(block % a.t_parts), reinterpret_cast<f32x4(*)[64]>(lds));
+      adapter_down<T, VEC, false, kGemmDownWaves>(a, block / a.t_parts, a.down_blocks / a.t_parts,
+                                                  (int)(block % a.t_parts),
+                                                  reinterpret_cast<f32x4(*)[64]>(stage0));
       return;
     }
     block -= a.down_blocks;
@@ -407,9 +477,11 @@ __global__ void __launch_bounds__(256) k_adapter_gemm(AdapterArgs a) {
   const int m = lane & 15, g = lane >> 4;
   const int64_t n = live_rows(a);
   const int outs = TR ? a.k : a.d, len = TR ? a.d : a.k;
-  const int tx = (int)(block % a.out_tiles);
-  const int64_t ty = block / a.out_tiles % a.row_tiles;
-  const int z = (int)(block / a.out_tiles / a.row_tiles);
+  const int64_t tiles = a.out_tiles * a.row_tiles;
+  const int z = (int)(block / tiles);
+  int tx;
+  int64_t ty;
+  tile_at(a, a.parts > 1 ? block - z * tiles : xcd_block(block, tiles), tx, ty);
   const int o0 = tx * TN;
   const int wo = (wave % G::WN) * NI * 16, wr = (wave / G::WN) * NJ * 16;
   const T* w = static_cast<const T*>(a.w);
@@ -417,102 +489,122 @@ __global__ void __launch_bounds__(256) k_adapter_gemm(AdapterArgs a) {
   const int blocks = (len + BK - 1) / BK;
   const int b0 = (int)((int64_t)z * blocks / a.parts);
   const int b1 = (int)((int64_t)(z + 1) * blocks / a.parts);
-  constexpr int XC = (G::XCH + 255) / 256, WC = G::WCH / 256;  // chunks per thread
-  static_assert(G::WCH % 256 == 0, "whole chunks per thread");
+  constexpr int XC = (G::XCH + TH - 1) / TH, WC = G::WCH / TH;  // chunks per thread
+  static_assert(G::WCH % TH == 0, "whole chunks per thread");
   const int64_t pos0 = ty * TM;
-  if (pos0 < n) {
-    f32x4 acc[NI][NJ];
+  if (pos0 >= n) return;
+  f32x4 acc[NI][NJ];
+#pragma unroll
+  for (int i = 0; i < NI; ++i)
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+  // this thread's chunks: LDS slot c = TH i + thread holds its row's chunk
+  // slot(row, c), as the slots are their own inverses
+  const T* xp[XC];
+  const T* wp[WC];
+#pragma unroll
+  for (int i = 0; i < XC; ++i) {
+    const int c = i * TH + threadIdx.x, r = c >> 3;
+    const int64_t pos = pos0 + r < n ? pos0 + r : n - 1;
+    xp[i] = xs + row_at(a, pos) * a.in_stride + G::xslot(r, c & 7) * E;
+  }
+#pragma unroll
+  for (int i = 0; i < WC; ++i) {
+    const int c = i * TH + threadIdx.x, r = c / G::RCH;
+    const int ch = G::wslot(r, c % G::RCH);
+    if constexpr (TR) {
+      const int o = o0 + ch * E < outs ? o0 + ch * E : 0;
+      wp[i] = w + (int64_t)r * a.k + o;
+    } else {
+      const int o = o0 + r < outs ? o0 + r : outs - 1;
+      wp[i] = w + (int64_t)o * a.k + ch * E;
+    }
+  }
+  auto whole = [&](int b) { return VEC && (b + 1) * BK <= len; };  // copied directly
+  auto copy = [&](int b, uint4* wl) __attribute__((always_inline)) {
+    uint4* xl = wl + G::WCH;
+    const int k0 = b * BK;
+#pragma unroll
+    for (int i = 0; i < WC; ++i)
+      copy_to_lds(wp[i] + (TR ? (int64_t)k0 * a.k : k0), wl + i * TH + wave * 64);
+#pragma unroll
+    for (int i = 0; i < XC; ++i)
+      if (G::XCH % TH == 0 || i * TH + wave * 64 < G::XCH)
+        copy_to_lds(xp[i] + k0, xl + i * TH + wave * 64);
+  };
+  auto stage = [&](int b, uint4* wl) __attribute__((always_inline)) {
+    if (whole(b)) return copy(b, wl);
+    uint4* xl = wl + G::WCH;
+    const int k0 = b * BK;
+#pragma unroll
+    for (int i = 0; i < WC; ++i) {
+      const int c = i * TH + threadIdx.x, r = c / G::RCH;
+      const int ch = G::wslot(r, c % G::RCH);
+      if constexpr (TR)
+        wl[c] = load_frag<T, VEC>(w + (int64_t)(k0 + r) * a.k + o0 + ch * E,
+                                  k0 + r < len ? outs - o0 - ch * E : 0);
+      else
+        wl[c] = load_frag<T, VEC>(wp[i] + k0, len - k0 - ch * E);
+    }
+#pragma unroll
+    for (int i = 0; i < XC; ++i) {
+      const int c = i * TH + threadIdx.x;
+      if (c < G::XCH) xl[c] = load_frag<T, VEC>(xp[i] + k0, len - k0 - G::xslot(c >> 3, c & 7) * E);
+    }
+  };
+  // Long reductions run in rounds of ST blocks that are all copied directly: a
+  // block is multiplied once it has landed (of the ST - 2 behind it each has at
+  // least kCopies copies under way) and the block before it is done with in
+  // every wave, while the block ST - 1 behind it is copied to that one's stage.
+  int b = b0;
+  const int bw = VEC ? min(b1, len / BK) : 0;  // blocks that are copied directly
+  if (bw - b0 >= 2 * ST - 1) {
+    auto step = [&](int c, const uint4* now, uint4* next) __attribute__((always_inline)) {
+      wait_copies<(ST - 2) * G::kCopies>();
+      copy(c + ST - 1, next);
+      __builtin_amdgcn_sched_barrier(0);  // the copies first
+      multiply<G, M, NI, NJ>(now, now + G::WCH, acc, wo, wr, m, g);
+    };
+    copy(b0, stage0);
+    copy(b0 + 1, stage1);
+    if constexpr (ST > 3) copy(b0 + 2, stage2);
+    for (; b + 2 * ST - 1 <= bw; b += ST) {
+      step(b, stage0, ST > 3 ? stage3 : stage2);
+      step(b + 1, stage1, stage0);
+      step(b + 2, stage2, stage1);
+      if constexpr (ST > 3) step(b + 3, stage3, stage2);
+    }
+  } else {
+    if (b0 < b1) stage(b0, stage0);
+    if (b0 + 1 < b1) stage(b0 + 1, stage1);
+    if (ST > 3 && b0 + 2 < b1) stage(b0 + 2, stage2);
+  }
+  // The last blocks, and short reductions: as above, each block as it may be
+  // loaded.
+  auto step = [&](int c, const uint4* now, uint4* next) __attribute__((always_inline)) {
+    if (c + ST - 2 < b1 && whole(c + ST - 2))
+      wait_copies<(ST - 2) * G::kCopies>();
+    else
+      wait_copies<0>();
+    if (c + ST - 1 < b1) stage(c + ST - 1, next);
+    multiply<G, M, NI, NJ>(now, now + G::WCH, acc, wo, wr, m, g);
+  };
+  for (; b < b1; b += ST) {
+    step(b, stage0, ST > 3 ? stage3 : stage2);
+    if (b + 1 < b1) step(b + 1, stage1, stage0);
+    if (b + 2 < b1) step(b + 2, stage2, stage1);
+    if (ST > 3 && b + 3 < b1) step(b + 3, stage3, stage2);
+  }
+  if (a.parts > 1) {
+    f32x4* out = reinterpret_cast<f32x4*>(a.part) +
+                 ((ty * a.out_tiles + tx) * a.parts + z) * (TN * TM / 4) + wave * NI * NJ * 64 +
+                 lane;
 #pragma unroll
     for (int i = 0; i < NI; ++i)
 #pragma unroll
-      for (int j = 0; j < NJ; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-    // this thread's chunks: LDS slot c = 256 i + thread holds its row's chunk
-    // slot(row, c), as the slots are their own inverses
-    const T* xp[XC];
-    const T* wp[WC];
-#pragma unroll
-    for (int i = 0; i < XC; ++i) {
-      const int c = i * 256 + threadIdx.x, r = c >> 3;
-      const int64_t pos = pos0 + r < n ? pos0 + r : n - 1;
-      xp[i] = xs + row_at(a, pos) * a.in_stride + G::xslot(r, c & 7) * E;
-    }
-#pragma unroll
-    for (int i = 0; i < WC; ++i) {
-      const int c = i * 256 + threadIdx.x, r = c / G::RCH;
-      const int ch = G::wslot(r, c % G::RCH);
-      if constexpr (TR) {
-        const int o = o0 + ch * E < outs ? o0 + ch * E : 0;
-        wp[i] = w + (int64_t)r * a.k + o;
-      } else {
-        const int o = o0 + r < outs ? o0 + r : outs - 1;
-        wp[i] = w + (int64_t)o * a.k + ch * E;
-      }
-    }
-    auto stage = [&](int b, int buf) {
-      uint4* wl = lds + buf * (G::WCH + G::XCH);
-      uint4* xl = wl + G::WCH;
-      const int k0 = b * BK;
-      if (VEC && k0 + BK <= len) {
-#pragma unroll
-        for (int i = 0; i < WC; ++i)
-          copy_to_lds(wp[i] + (TR ? (int64_t)k0 * a.k : k0), wl + i * 256 + wave * 64);
-#pragma unroll
-        for (int i = 0; i < XC; ++i)
-          if (G::XCH % 256 == 0 || i * 256 + wave * 64 < G::XCH)
-            copy_to_lds(xp[i] + k0, xl + i * 256 + wave * 64);
-        return;
-      }
-#pragma unroll
-      for (int i = 0; i < WC; ++i) {
-        const int c = i * 256 + threadIdx.x, r = c / G::RCH;
-        const int ch = G::wslot(r, c % G::RCH);
-        if constexpr (TR)
-          wl[c] = load_frag<T, VEC>(w + (int64_t)(k0 + r) * a.k + o0 + ch * E,
-                                    k0 + r < len ? outs - o0 - ch * E : 0);
-        else
-          wl[c] = load_frag<T, VEC>(wp[i] + k0, len - k0 - ch * E);
-      }
-#pragma unroll
-      for (int i = 0; i < XC; ++i) {
-        const int c = i * 256 + threadIdx.x;
-        if (c < G::XCH) xl[c] = load_frag<T, VEC>(xp[i] + k0, len - k0 - G::xslot(c >> 3, c & 7) * E);
-      }
-    };
-    if (b0 < b1) stage(b0, 0);
-    for (int b = b0; b < b1; ++b) {
-      // this block's copies have landed, and every wave is done with the other buffer
-      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-      __syncthreads();
-      if (b + 1 < b1) stage(b + 1, (b + 1 - b0) & 1);
-      const uint4* wl = lds + ((b - b0) & 1) * (G::WCH + G::XCH);
-      const uint4* xl = wl + G::WCH;
-#pragma unroll
-      for (int s = 0; s < 2; ++s) {
-        uint4 av[NI], bv[NJ];
-#pragma unroll
-        for (int i = 0; i < NI; ++i) av[i] = G::wfrag(wl, wo + i * 16, s, m, g);
-#pragma unroll
-        for (int j = 0; j < NJ; ++j) {
-          const int r = wr + j * 16 + m;
-          bv[j] = xl[r * 8 + G::xslot(r, 4 * s + g)];
-        }
-#pragma unroll
-        for (int i = 0; i < NI; ++i)
-#pragma unroll
-          for (int j = 0; j < NJ; ++j) acc[i][j] = M::mma(av[i], bv[j], acc[i][j]);
-      }
-    }
-    if (a.parts > 1) {
-      f32x4* out = reinterpret_cast<f32x4*>(a.part) +
-                   ((ty * a.out_tiles + tx) * a.parts + z) * (TN * TM / 4) + wave * NI * NJ * 64 +
-                   lane;
-#pragma unroll
-      for (int i = 0; i < NI; ++i)
-#pragma unroll
-        for (int j = 0; j < NJ; ++j) out[(i * NJ + j) * 64] = acc[i][j];
-    } else {
-      adapter_epilogue<T, TR, NI, NJ>(a, acc, o0 + wo, pos0 + wr, n, m, g);
-    }
+      for (int j = 0; j < NJ; ++j) out[(i * NJ + j) * 64] = acc[i][j];
+  } else {
+    adapter_epilogue<T, TR, NI, NJ, 1>(a, acc, o0 + wo, pos0 + wr, n, m, g);
   }
 }
 
@@ -535,7 +627,7 @@ __global__ void __launch_bounds__(256) k_adapter_join(AdapterArgs a) {
   f32x4 acc[1][1] = {{in[0]}};
 #pragma unroll 8
   for (int h = 1; h < a.parts; ++h) acc[0][0] += in[(int64_t)h * (TN * TM / 4)];
-  adapter_epilogue<T, TR, 1, 1>(a, acc, o0, pos0, n, lane & 15, lane >> 4);
+  adapter_epilogue<T, TR, 1, 1, kMaxDownParts>(a, acc, o0, pos0, n, lane & 15, lane >> 4);
 }
 
 // The rows of each adapter in ascending order: rows[off[p] .. off[p + 1]), and
@@ -587,16 +679,15 @@ __global__ void __launch_bounds__(64 * kListWaves) k_adapter_list(AdapterArgs a,
 // waves share them and add their sums through LDS; the other waves of a
 // workgroup take other columns.
 struct GradArgs {
-  const float* t[2];        // u, t: [parts][max_rows][rp]
+  const float* t[2];        // u, t
   const void* v[2];         // x, dy
   float* out[2];            // da, db
   int64_t v_stride[2];
-  int32_t parts[2], cols[2];
+  int32_t cols[2];
   int32_t vec[2];           // a lane's columns are one aligned load
   int32_t blocks0;          // workgroups per adapter that take da's columns
   const int32_t* off;
   const int32_t* rows;
-  int64_t max_rows;
   int32_t rank, rp;
 };
 
@@ -609,7 +700,7 @@ __global__ void __launch_bounds__(512) k_adapter_grad(GradArgs a) {
   const int m = lane & 15, g = lane >> 4, rw = wave % RW;
   const int which = (int)blockIdx.x >= a.blocks0, p = blockIdx.y;
   const int blk = (int)blockIdx.x - (which ? a.blocks0 : 0);
-  const int cols = which ? a.cols[1] : a.cols[0], parts = which ? a.parts[1] : a.parts[0];
+  const int cols = which ? a.cols[1] : a.cols[0];
   const bool vec = (which ? a.vec[1] : a.vec[0]) != 0;
   const int64_t stride = which ? a.v_stride[1] : a.v_stride[0];
   const float* t = which ? a.t[1] : a.t[0];
@@ -621,19 +712,24 @@ __global__ void __launch_bounds__(512) k_adapter_grad(GradArgs a) {
     f32x4 acc[CPL];
 #pragma unroll
     for (int i = 0; i < CPL; ++i) acc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+    int32_t row[4];  // of the next 16 rows, -1 behind the last
+    auto next_rows = [&](int32_t r) {
+#pragma unroll
+      for (int s = 0; s < 4; ++s) row[s] = r + 4 * g + s < e ? a.rows[r + 4 * g + s] : -1;
+    };
+    next_rows(b + rw * 16);
     for (int32_t r = b + rw * 16; r < e; r += 16 * RW) {
       f32x4 uv;
       uint4 xv[4];
 #pragma unroll
       for (int s = 0; s < 4; ++s) {
-        const int32_t at = r + 4 * g + s;
-        const bool in = at < e;
-        const T* x = v + (in ? a.rows[at] : 0) * stride + c;
+        const bool in = row[s] >= 0;
+        const T* x = v + (in ? row[s] : 0) * stride + c;
         xv[s] = vec ? load_frag<T, true>(x, in ? cols - c : 0)
                     : load_frag<T, false>(x, in ? cols - c : 0);
-        uv[s] = 0.0f;
-        for (int h = 0; in && h < parts; ++h) uv[s] += t[(h * a.max_rows + at) * a.rp + j0 + m];
+        uv[s] = in ? t[(int64_t)(r + 4 * g + s) * a.rp + j0 + m] : 0.0f;
       }
+      next_rows(r + 16 * RW);
 #pragma unroll
       for (int i = 0; i < CPL; ++i) {
         f32x4 xi;
@@ -648,10 +744,10 @@ __global__ void __launch_bounds__(512) k_adapter_grad(GradArgs a) {
       for (int i = 0; i < CPL; ++i) red[wave][i][lane] = acc[i];
       __syncthreads();
       if (rw == 0) {
+#pragma unroll 1
+        for (int w = 1; w < RW; ++w)
 #pragma unroll
-        for (int i = 0; i < CPL; ++i)
-#pragma unroll
-          for (int w = 1; w < RW; ++w) acc[i] += red[wave + w][i][lane];
+          for (int i = 0; i < CPL; ++i) acc[i] += red[wave + w][i][lane];
       }
     }
     if (rw == 0) {
@@ -705,10 +801,9 @@ GemmPlan plan_gemm(int64_t max_rows, int64_t outs, int64_t len, int64_t es) {
   auto tiles = [&](int64_t tn, int64_t tm) {
     return (outs + tn - 1) / tn * ((max_rows + tm - 1) / tm);
   };
-  p.tn = 128;
-  if (max_rows <= 16) p.tm = 16;
-  else if (tiles(128, 128) >= 2 * kNumCU) p.tm = 128;
-  else p.tm = 64;
+  const bool big = tiles(256, 128) >= kNumCU;
+  p.tn = big ? 256 : 128;
+  p.tm = big ? 128 : max_rows <= 16 ? 16 : 64;
   const int64_t t = tiles(p.tn, p.tm), blocks = (len * es + 127) / 128;
   // parts for about two workgroups per CU, each of at least four blocks
   int64_t parts = t > 0 && t < kNumCU ? 2 * kNumCU / t : 1;
@@ -724,14 +819,14 @@ size_t gemm_part_bytes(const GemmPlan& p, int64_t max_rows, int64_t outs) {
          p.parts * 4;
 }
 
-// Parts of the rank-wide rows' reduction: about four workgroups per CU, each
-// wave of at least two steps of 64 bytes.
+// Parts of the rank-wide rows' reduction beside a split product: about four
+// workgroups per CU, each wave of at least two steps of 64 bytes.
 int32_t down_parts(int64_t max_rows, int64_t len, int64_t es) {
   const int64_t tiles = (max_rows + 15) / 16;
   int64_t parts = tiles > 0 ? 4 * kNumCU / tiles : 1;
-  const int64_t most = len * es / (64 * 2 * kDownWaves);
+  const int64_t most = len * es / (64 * 2 * kGemmDownWaves);
   if (parts > most) parts = most;
-  if (parts > 8) parts = 8;
+  if (parts > kMaxDownParts) parts = kMaxDownParts;
   return parts < 1 ? 1 : (int32_t)parts;
 }
 
@@ -743,7 +838,7 @@ constexpr int64_t kListRows = 256;
 // partial sums, and the rows by adapter.
 struct AdapterLayout {
   size_t t, u, part, off, rows, total;
-  int32_t t_parts, u_parts;
+  int32_t t_parts;
   GemmPlan g;
   bool list;
 };
@@ -758,12 +853,11 @@ AdapterLayout adapter_layout(const nsc_adapter_desc& d, int64_t max_rows, bool b
   };
   const int64_t es = type_bytes(d.dtype);
   const size_t rp = align_up(d.rank, 16);
-  L.t_parts = down_parts(max_rows, d.k, es);
-  L.u_parts = down_parts(max_rows, d.d, es);
   L.g = backward ? plan_gemm(max_rows, d.k, d.d, es) : plan_gemm(max_rows, d.d, d.k, es);
+  L.t_parts = backward || L.g.parts == 1 ? 1 : down_parts(max_rows, d.k, es);
   L.list = backward || max_rows >= kListRows;
   L.t = take((size_t)max_rows * rp * 4 * L.t_parts);
-  if (backward) L.u = take((size_t)max_rows * rp * 4 * L.u_parts);
+  if (backward) L.u = take((size_t)max_rows * rp * 4);
   L.part = take(gemm_part_bytes(L.g, max_rows, backward ? d.k : d.d));
   if (L.list) {
     L.off = take(((size_t)d.n_adapters + 1) * 4);
@@ -789,7 +883,7 @@ template <typename T>
 int launch_down(const AdapterArgs& a, bool vec, bool b, hipStream_t st) {
   int64_t grid = (a.max_rows + 15) / 16;
   if (grid > 16 * kNumCU) grid = 16 * kNumCU;
-  const dim3 g((unsigned)grid, (unsigned)a.t_parts), t(64 * kDownWaves);
+  const dim3 g((unsigned)grid), t(64 * kDownWaves);
   if (b)
     hipLaunchKernelGGL((k_adapter_down<T, false, true>), g, t, 0, st, a);
   else if (vec)
@@ -800,9 +894,8 @@ int launch_down(const AdapterArgs& a, bool vec, bool b, hipStream_t st) {
   return NSC_OK;
 }
 
-template <typename T, bool VEC, bool TR, int TM>
+template <typename T, bool VEC, bool TR, int TN, int TM>
 int launch_tiles(AdapterArgs a, hipStream_t st) {
-  constexpr int TN = 128;
   using G = Gemm<T, TR, TN, TM>;
   a.out_tiles = ((TR ? a.k : a.d) + TN - 1) / TN;
   a.row_tiles = (a.max_rows + TM - 1) / TM;
@@ -810,40 +903,49 @@ int launch_tiles(AdapterArgs a, hipStream_t st) {
   if (grid > 0x7FFFFFFF)
     return fail(NSC_E_SHAPE, "%lld rows onto %d outputs are more tiles than a launch holds",
                 (long long)a.max_rows, TR ? a.k : a.d);
-  hipLaunchKernelGGL((k_adapter_gemm<T, VEC, TR, TN, TM>), dim3((unsigned)grid), dim3(256),
-                     G::kLds, st, a);
+  hipLaunchKernelGGL((k_adapter_gemm<T, VEC, TR, TN, TM>), dim3((unsigned)grid),
+                     dim3(G::kThreads), 0, st, a);
   NSC_CHECK_LAUNCH("k_adapter_gemm");
-  if (a.parts > 1) {
-    hipLaunchKernelGGL((k_adapter_join<T, TR, TN, TM>), dim3((unsigned)(tiles * (TN * TM / 1024))),
-                       dim3(256), 0, st, a);
-    NSC_CHECK_LAUNCH("k_adapter_join");
+  if constexpr (TN < 256) {
+    if (a.parts > 1) {
+      hipLaunchKernelGGL((k_adapter_join<T, TR, TN, TM>),
+                         dim3((unsigned)(tiles * (TN * TM / 1024))), dim3(256), 0, st, a);
+      NSC_CHECK_LAUNCH("k_adapter_join");
+    }
   }
   return NSC_OK;
 }
 
-template <typename T, bool TR>
-int launch_gemm(const AdapterArgs& a, const GemmPlan& p, bool vec, hipStream_t st) {
-  if (p.tm == 128)
-    return vec ? launch_tiles<T, true, TR, 128>(a, st) : launch_tiles<T, false, TR, 128>(a, st);
-  if (p.tm == 64)
-    return vec ? launch_tiles<T, true, TR, 64>(a, st) : launch_tiles<T, false, TR, 64>(a, st);
-  return vec ? launch_tiles<T, true, TR, 16>(a, st) : launch_tiles<T, false, TR, 16>(a, st);
+template <typename T, bool VEC, bool TR>
+int launch_plan(const AdapterArgs& a, const GemmPlan& p, hipStream_t st) {
+  if (p.tn == 256) return launch_tiles<T, VEC, TR, 256, 128>(a, st);
+  if (p.tm == 64) return launch_tiles<T, VEC, TR, 128, 64>(a, st);
+  return launch_tiles<T, VEC, TR, 128, 16>(a, st);
 }
 
-// Eight waves share an adapter's rows where there are many of them on average,
-// else each takes columns of its own.
+template <typename T, bool TR>
+int launch_gemm(const AdapterArgs& a, const GemmPlan& p, bool vec, hipStream_t st) {
+  return vec ? launch_plan<T, true, TR>(a, p, st) : launch_plan<T, false, TR>(a, p, st);
+}
+
+// Waves share an adapter's rows where its columns alone make too few of them
+// (about two per SIMD) and it has two steps of 16 rows for each on average.
 template <typename T>
-int launch_grad(GradArgs a, int32_t n_adapters, hipStream_t st) {
+int launch_grad(GradArgs a, int32_t n_adapters, int64_t max_rows, hipStream_t st) {
   constexpr int CPL = 16 / sizeof(T);
-  const bool share = a.max_rows / n_adapters >= 512;
-  const int32_t width = 16 * CPL * (share ? 1 : 8);
+  const int64_t waves = ((int64_t)a.cols[0] + a.cols[1]) / (16 * CPL) * n_adapters;
+  int rw = 1;
+  while (rw < 8 && waves * rw < 8 * kNumCU && max_rows / n_adapters >= 2 * 16 * 2 * rw) rw *= 2;
+  const int32_t width = 16 * CPL * (8 / rw);
   a.blocks0 = (a.cols[0] + width - 1) / width;
   const dim3 g((unsigned)(a.blocks0 + (a.cols[1] + width - 1) / width), (unsigned)n_adapters),
       t(512);
-  if (share)
-    hipLaunchKernelGGL((k_adapter_grad<T, 8>), g, t, 0, st, a);
-  else
-    hipLaunchKernelGGL((k_adapter_grad<T, 1>), g, t, 0, st, a);
+  switch (rw) {
+    case 1: hipLaunchKernelGGL((k_adapter_grad<T, 1>), g, t, 0, st, a); break;
+    case 2: hipLaunchKernelGGL((k_adapter_grad<T, 2>), g, t, 0, st, a); break;
+    case 4: hipLaunchKernelGGL((k_adapter_grad<T, 4>), g, t, 0, st, a); break;
+    default: hipLaunchKernelGGL((k_adapter_grad<T, 8>), g, t, 0, st, a); break;
+  }
   NSC_CHECK_LAUNCH("k_adapter_grad");
   return NSC_OK;
 }
@@ -916,7 +1018,7 @@ int backward(const nsc_adapter_desc& d, AdapterArgs a, const void* x, const void
     a.x = x;
     a.in_stride = d.x_stride;
     a.t = t;
-    a.t_parts = L.t_parts;
+    a.t_parts = 1;
     if (int rc = launch_down<T>(
             a, !misaligned(x, 16) && !misaligned(a.a, 16) && d.k % E == 0 && d.x_stride % E == 0,
             false, st))
@@ -924,7 +1026,6 @@ int backward(const nsc_adapter_desc& d, AdapterArgs a, const void* x, const void
     a.x = dy;
     a.in_stride = d.y_stride;
     a.t = u;
-    a.t_parts = L.u_parts;
     if (int rc = launch_down<T>(a, false, true, st)) return rc;
     if (dx) {
       a.out = dx;
@@ -940,7 +1041,6 @@ int backward(const nsc_adapter_desc& d, AdapterArgs a, const void* x, const void
   GradArgs g{};
   g.off = off;
   g.rows = rows;
-  g.max_rows = a.max_rows;
   g.rank = a.rank;
   g.rp = a.rp;
   const void* v[2] = {x, dy};
@@ -948,14 +1048,13 @@ int backward(const nsc_adapter_desc& d, AdapterArgs a, const void* x, const void
   const int32_t cols[2] = {d.k, d.d};
   for (int i = 0; i < 2; ++i) {
     g.t[i] = i ? t : u;
-    g.parts[i] = i ? L.t_parts : L.u_parts;
     g.v[i] = v[i];
     g.v_stride[i] = strides[i];
     g.cols[i] = cols[i];
     g.vec[i] = !misaligned(v[i], 16) && strides[i] % E == 0 && cols[i] % E == 0;
     g.out[i] = i ? db : da;
   }
-  return launch_grad<T>(g, d.n_adapters, st);
+  return launch_grad<T>(g, d.n_adapters, a.max_rows, st);
 }
 
 }  // namespace
