@@ -126,25 +126,49 @@ __device__ __forceinline__ uint32_t rows_of(int mine, int p) {
   return (uint32_t)__ballot(mine == p) & 0xFFFFu;
 }
 
-// Rank-wide rows of 16 positions: a workgroup per (tile, part of the
-// reduction), whose waves split the part and add their sums through LDS.  A
-// lane keeps the products of its own row's adapter.  B = false: t = scale x a^T
-// over k; B = true: u = scale dy b over d, whose values lie rank apart.
-constexpr int kDownSteps = 4;  // steps whose loads are in flight together
+// 16 bytes per lane from memory straight to LDS, at the wave's lds + 16 * lane.
+__device__ __forceinline__ void copy_to_lds(const void* from, void* lds) {
+  __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from,
+                                   (__attribute__((address_space(3))) void*)lds, 16, 0, 0);
+}
 
-template <typename T, bool VEC, bool B, int W>
+// Waits until at most N of the wave's copies are under way and its LDS
+// accesses are done.  (The builtin's wait is one that the compiler counts with.)
+template <int N>
+__device__ __forceinline__ void wait_copies() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt((N & 15) | (N >> 4) << 14 | 0x70);  // vmcnt(N) lgkmcnt(0)
+  asm volatile("" ::: "memory");
+}
+
+// Chunk c of 128-byte row r lies at chunk slot(r, c) of its row in LDS, so that
+// 16 lanes that read one chunk of 16 rows fall on different banks.
+__device__ __forceinline__ int row_slot(int r, int c) { return c ^ (r & 7); }
+
+// Rank-wide rows of 16 positions: a workgroup per (tile, part of the
+// reduction), whose W waves split the part and add their sums through LDS.
+// Each wave copies 128 bytes of its 16 rows and of an adapter's 16 rank rows
+// at a time to LDS of its own, two such chunks ahead (loaded as fragments, 16
+// lanes read 16 rows and a CU takes 7 bytes a cycle: 1,501 rows of 9,216 fp32
+// 85 us), adapter by adapter among the rows; a lane keeps the products of its
+// own row's adapter.  What is not whole aligned chunks is loaded as fragments.
+template <typename T, bool VEC, int W>
 __device__ __forceinline__ void adapter_down(const AdapterArgs& a, int64_t block, int64_t blocks,
-                                             int part, f32x4 (*red)[64]) {
+                                             int part, uint4* stage0, uint4* stage1, uint4* stage2,
+                                             f32x4 (*red)[64]) {
   using M = Mma<T>;
-  constexpr int KS = B ? 16 : M::KS, S = kDownSteps;
+  constexpr int E = M::E, BK = 2 * M::KS;
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int m = lane & 15, g = lane >> 4;
   const int64_t n = live_rows(a);
-  const int len = B ? a.d : a.k;
-  const int steps = (len + KS - 1) / KS, parts = a.t_parts * W;
-  const int s0 = (int)((int64_t)(part * W + wave) * steps / parts);
-  const int s1 = (int)((int64_t)(part * W + wave + 1) * steps / parts);
+  const int whole = VEC ? a.k / BK : 0;  // chunks that are copied
+  const int parts = a.t_parts * W, me = part * W + wave;
+  const int c0 = (int)((int64_t)me * whole / parts), c1 = (int)((int64_t)(me + 1) * whole / parts);
+  // the values behind them, by steps
+  const int steps = (a.k - whole * BK + M::KS - 1) / M::KS;
+  const int s0 = (int)((int64_t)me * steps / parts), s1 = (int)((int64_t)(me + 1) * steps / parts);
+  const int cr = lane >> 3, cs = row_slot(cr, lane & 7) * E;  // a copy's row (and + 8), values
   for (int64_t pos0 = block * 16; pos0 < n; pos0 += blocks * 16) {
     const bool in = pos0 + m < n;
     const int64_t row = row_at(a, in ? pos0 + m : n - 1);
@@ -152,60 +176,78 @@ __device__ __forceinline__ void adapter_down(const AdapterArgs& a, int64_t block
     const float scale = mine != INT_MAX ? a.scale[mine] : 0.0f;
     const uint32_t some = with_adapter(mine);
     const T* x = static_cast<const T*>(a.x) + row * a.in_stride;
+    const T* xc[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int64_t pos = pos0 + cr + 8 * h;
+      xc[h] = static_cast<const T*>(a.x) + row_at(a, pos < n ? pos : n - 1) * a.in_stride + cs;
+    }
     for (int j0 = 0; j0 < a.rp; j0 += 16) {
       f32x4 out = {0.f, 0.f, 0.f, 0.f};
-      const int j = j0 + m;
-      if (some)
-        for (int s = s0; s < s1; s += S) {
-          typename std::conditional<B, f32x4, uint4>::type xv[S], wv[S];
-          auto inside = [&](int u) {  // values from step s + u's first of this lane on
-            return s + u < s1 ? len - (s + u) * KS - (B ? 4 : M::E) * g : 0;
-          };
-          auto load_w = [&](int p) {
-            if constexpr (B) {
-              const T* b = static_cast<const T*>(a.b) + (int64_t)p * a.d * a.rank + j;
+      int items = 0;  // (adapter, chunk) pairs
+      for (uint32_t t = some; t; items += c1 - c0) t &= ~rows_of(mine, pick_adapter(mine, t));
+      if (c1 == c0) items = 0;
+      if (items) {
+        uint32_t ftodo = some, todo = some;
+        int fp = pick_adapter(mine, some), fc = c0, p = fp, c = c0;
+        int64_t ac[2];
 #pragma unroll
-              for (int u = 0; u < S; ++u) {
-                const int k = (s + u) * KS + 4 * g, left = j < a.rank ? inside(u) : 0;
+        for (int h = 0; h < 2; ++h) ac[h] = (int64_t)min(j0 + cr + 8 * h, a.rank - 1) * a.k + cs;
+        auto issue = [&](uint4* st) __attribute__((always_inline)) {
+          const T* ap = static_cast<const T*>(a.a) + (int64_t)fp * a.rank * a.k + fc * BK;
 #pragma unroll
-                for (int e = 0; e < 4; ++e)
-                  wv[u][e] = e < left ? (float)b[(int64_t)(k + e) * a.rank] : 0.0f;
-              }
-            } else {
-              const T* ar = static_cast<const T*>(a.a) + ((int64_t)p * a.rank + j) * a.k;
+          for (int h = 0; h < 2; ++h) copy_to_lds(xc[h] + fc * BK, st + wave * 256 + h * 64);
 #pragma unroll
-              for (int u = 0; u < S; ++u)
-                wv[u] = load_frag<T, VEC>(ar + (s + u) * KS + M::E * g, j < a.rank ? inside(u) : 0);
-            }
-          };
-          uint32_t todo = some;
-          int p = pick_adapter(mine, todo);
-          load_w(p);
-#pragma unroll
-          for (int u = 0; u < S; ++u) {
-            if constexpr (B)
-              xv[u] = load4(x + (s + u) * KS + 4 * g, inside(u));
-            else
-              xv[u] = load_frag<T, VEC>(x + (s + u) * KS + M::E * g, inside(u));
+          for (int h = 0; h < 2; ++h) copy_to_lds(ap + ac[h], st + wave * 256 + 128 + h * 64);
+          if (++fc == c1) {
+            fc = c0;
+            ftodo &= ~rows_of(mine, fp);
+            if (ftodo) fp = pick_adapter(mine, ftodo);
           }
-          for (;;) {
-            f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+        };
+        f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+        auto step = [&](int i, const uint4* now, uint4* next) __attribute__((always_inline)) {
+          if (i + 1 < items)
+            wait_copies<4>();
+          else
+            wait_copies<0>();
+          if (i + 2 < items) issue(next);
 #pragma unroll
-            for (int u = 0; u < S; ++u) {
-              if constexpr (B)
-                acc = mma_f32(wv[u], xv[u], acc);
-              else
-                acc = M::mma(wv[u], xv[u], acc);
-            }
-            const bool hit = mine == p;
+          for (int s = 0; s < 2; ++s) {
+            const uint4* at = now + wave * 256 + m * 8 + row_slot(m, 4 * s + g);
+            acc = M::mma(at[128], at[0], acc);
+          }
+          if (++c == c1) {
+            c = c0;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) out[e] += mine == p ? acc[e] : 0.0f;
+            acc = f32x4{0.f, 0.f, 0.f, 0.f};
             todo &= ~rows_of(mine, p);
-            if (todo) {  // the next adapter's values while this one's products finish
-              p = pick_adapter(mine, todo);
-              load_w(p);
-            }
-            if (hit) out += acc;
-            if (!todo) break;
+            if (todo) p = pick_adapter(mine, todo);
           }
+        };
+        wait_copies<0>();  // of the loads above, not of the copies in the loop
+        issue(stage0);
+        issue(stage1);  // behind a single item: that item's again
+        for (int i = 0; i < items; i += 3) {
+          step(i, stage0, stage2);
+          if (i + 1 < items) step(i + 1, stage1, stage0);
+          if (i + 2 < items) step(i + 2, stage2, stage1);
+        }
+      }
+      if (s0 < s1)
+        for (uint32_t todo = some; todo;) {
+          const int p = pick_adapter(mine, todo), j = j0 + m;
+          todo &= ~rows_of(mine, p);
+          const T* ap = static_cast<const T*>(a.a) + ((int64_t)p * a.rank + j) * a.k;
+          f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+          for (int s = s0; s < s1; ++s) {
+            const int k = whole * BK + s * M::KS + E * g;
+            const uint4 av = load_frag<T, VEC>(ap + k, j < a.rank ? a.k - k : 0);
+            acc = M::mma(av, load_frag<T, VEC>(x + k, a.k - k), acc);
+          }
+#pragma unroll
+          for (int e = 0; e < 4; ++e) out[e] += mine == p ? acc[e] : 0.0f;
         }
       __syncthreads();  // red is read before it is written again
       red[wave][lane] = out;
@@ -213,21 +255,36 @@ __device__ __forceinline__ void adapter_down(const AdapterArgs& a, int64_t block
       if (wave == 0 && in) {
 #pragma unroll
         for (int w = 1; w < W; ++w) out += red[w][lane];
-        *reinterpret_cast<f32x4*>(a.t + (part * a.max_rows + pos0 + m) * a.rp + j0 + 4 * g) =
-            out * scale;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) out[e] = j0 + 4 * g + e < a.rank ? out[e] * scale : 0.0f;
+        *reinterpret_cast<f32x4*>(a.t + (part * a.max_rows + pos0 + m) * a.rp + j0 + 4 * g) = out;
       }
     }
   }
 }
 
-constexpr int kDownWaves = 16;  // alone in a launch; kGemmDownWaves beside the product
-constexpr int kGemmDownWaves = 4;
-constexpr int kMaxDownParts = 8;
+// The rank-wide rows alone in a launch: of one reduction (t of x and a), or of
+// two (and u of dy and the transposed b).
+constexpr int kDownWaves = 8, kGemmDownWaves = 4;
+constexpr int kMaxParts = 4, kMaxJoinParts = 8;  // of their reduction; beside a split product
 
-template <typename T, bool VEC, bool B>
-__global__ void __launch_bounds__(64 * kDownWaves) k_adapter_down(AdapterArgs a) {
+struct DownArgs {
+  AdapterArgs of[2];
+  int32_t vec[2];
+};
+
+template <typename T>
+__global__ void __launch_bounds__(64 * kDownWaves) k_adapter_down(DownArgs d) {
+  __shared__ uint4 stage0[kDownWaves * 256], stage1[kDownWaves * 256], stage2[kDownWaves * 256];
   __shared__ f32x4 red[kDownWaves][64];
-  adapter_down<T, VEC, B, kDownWaves>(a, blockIdx.x, gridDim.x, 0, red);
+  const AdapterArgs& a = blockIdx.z ? d.of[1] : d.of[0];
+  if ((int)blockIdx.y >= a.t_parts) return;
+  if (blockIdx.z ? d.vec[1] : d.vec[0])
+    adapter_down<T, true, kDownWaves>(a, blockIdx.x, gridDim.x, blockIdx.y, stage0, stage1, stage2,
+                                      red);
+  else
+    adapter_down<T, false, kDownWaves>(a, blockIdx.x, gridDim.x, blockIdx.y, stage0, stage1,
+                                       stage2, red);
 }
 
 // The shared product with the rank-wide rows' in its epilogue, in tiles of TN
@@ -260,7 +317,7 @@ struct Gemm {
   // a read fall on different banks: x and w by rows (16 lanes read one chunk
   // of 16 rows), and w transposed (16-bit: 32-byte blocks of rows 8 g + 0..3
   // of 2 lane groups at once; 32-bit: 64-byte blocks of rows 4 g of 4).
-  static __device__ __forceinline__ int xslot(int r, int c) { return c ^ (r & 7); }
+  static __device__ __forceinline__ int xslot(int r, int c) { return row_slot(r, c); }
   static __device__ __forceinline__ int wslot(int r, int c) {
     if constexpr (!TR) return c ^ (r & 7);
     if constexpr (sizeof(T) == 2) return c ^ ((((r & 3) | ((r >> 1) & 4)) << 1) & (RCH - 1));
@@ -293,12 +350,6 @@ struct Gemm {
     }
   }
 };
-
-// 16 bytes per lane from memory straight to LDS, at the wave's lds + 16 * lane.
-__device__ __forceinline__ void copy_to_lds(const void* from, void* lds) {
-  __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from,
-                                   (__attribute__((address_space(3))) void*)lds, 16, 0, 0);
-}
 
 // Adds the rank-wide rows' products and the bias to outputs o0 .. of positions
 // pos0 .. and stores them.  TP: most parts of the rank-wide rows.
@@ -335,13 +386,10 @@ __device__ __forceinline__ void adapter_epilogue(const AdapterArgs& a, f32x4 (&a
         for (int h = 0; h < TP; ++h) tv[j] += v[h];
       }
     }
-    for (;;) {
-      int p = INT_MAX;
-#pragma unroll
-      for (int j = 0; j < NJ; ++j)
-        if (p == INT_MAX && todo[j]) p = pick_adapter(mine[j], todo[j]);
-      if (p == INT_MAX) break;
-      f32x4 bv[NI];
+    // PB adapters at a time, whose loads are under way together: a join's waves
+    // have one block each and wait for little else
+    constexpr int PB = NI * NJ == 1 ? 4 : 1;
+    auto load_b = [&](int p, f32x4 (&bv)[NI]) __attribute__((always_inline)) {
 #pragma unroll
       for (int i = 0; i < NI; ++i) {
         const int o = o0 + i * 16 + m;
@@ -366,12 +414,12 @@ __device__ __forceinline__ void adapter_epilogue(const AdapterArgs& a, f32x4 (&a
           }
         }
       }
+    };
+    auto add_b = [&](int p, const f32x4 (&bv)[NI]) __attribute__((always_inline)) {
 #pragma unroll
       for (int j = 0; j < NJ; ++j) {
         __builtin_amdgcn_sched_barrier(0);
-        const uint32_t hit = rows_of(mine[j], p);
-        if (hit) {
-          todo[j] &= ~hit;
+        if (rows_of(mine[j], p)) {
 #pragma unroll
           for (int i = 0; i < NI; ++i) {
             const f32x4 add = mma_f32(bv[i], tv[j], f32x4{0.f, 0.f, 0.f, 0.f});
@@ -380,6 +428,30 @@ __device__ __forceinline__ void adapter_epilogue(const AdapterArgs& a, f32x4 (&a
           }
         }
       }
+    };
+    auto next = [&]() __attribute__((always_inline)) {
+      int p = INT_MAX;
+#pragma unroll
+      for (int j = 0; j < NJ; ++j)
+        if (p == INT_MAX && todo[j]) p = pick_adapter(mine[j], todo[j]);
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) todo[j] &= ~rows_of(mine[j], p);
+      return p;
+    };
+    for (int p = next(); p != INT_MAX; p = next()) {
+      f32x4 bv[PB][NI];
+      int ps[PB];
+      ps[0] = p;
+      load_b(p, bv[0]);
+#pragma unroll
+      for (int k = 1; k < PB; ++k) {
+        ps[k] = next();
+        if (ps[k] != INT_MAX) load_b(ps[k], bv[k]);
+      }
+      add_b(p, bv[0]);
+#pragma unroll
+      for (int k = 1; k < PB; ++k)
+        if (ps[k] != INT_MAX) add_b(ps[k], bv[k]);
     }
   }
   f32x4 bias[NI];
@@ -408,17 +480,6 @@ __device__ __forceinline__ void adapter_epilogue(const AdapterArgs& a, f32x4 (&a
       }
     }
   }
-}
-
-// Waits until at most N of the wave's copies are under way and its LDS writes
-// have landed, then for the workgroup's other waves.
-template <int N>
-__device__ __forceinline__ void wait_copies() {
-  asm volatile("" ::: "memory");
-  // vmcnt(N) lgkmcnt(0); the builtin's wait is one the compiler counts with
-  __builtin_amdgcn_s_waitcnt((N & 15) | (N >> 4) << 14 | 0x70);
-  __builtin_amdgcn_s_barrier();
-  asm volatile("" ::: "memory");
 }
 
 // A block's products from its tiles.
@@ -465,9 +526,10 @@ __global__ void __launch_bounds__(TN >= 256 ? 512 : 256) k_adapter_gemm(AdapterA
   int64_t block = blockIdx.x;
   if constexpr (!TR && TN < 256) {  // a call whose product is split takes its rank-wide rows here
     if (block < a.down_blocks) {
-      adapter_down<T, VEC, false, kGemmDownWaves>(a, block / a.t_parts, a.down_blocks / a.t_parts,
-                                                  (int)(block % a.t_parts),
-                                                  reinterpret_cast<f32x4(*)[64]>(stage0));
+      static_assert(kStage >= kGemmDownWaves * 256 && kGemmDownWaves * 64 == TH, "in the stages");
+      adapter_down<T, VEC, kGemmDownWaves>(a, block / a.t_parts, a.down_blocks / a.t_parts,
+                                           (int)(block % a.t_parts), stage0, stage1, stage2,
+                                           reinterpret_cast<f32x4(*)[64]>(stage0));
       return;
     }
     block -= a.down_blocks;
@@ -561,6 +623,7 @@ __global__ void __launch_bounds__(TN >= 256 ? 512 : 256) k_adapter_gemm(AdapterA
   if (bw - b0 >= 2 * ST - 1) {
     auto step = [&](int c, const uint4* now, uint4* next) __attribute__((always_inline)) {
       wait_copies<(ST - 2) * G::kCopies>();
+      __builtin_amdgcn_s_barrier();
       copy(c + ST - 1, next);
       __builtin_amdgcn_sched_barrier(0);  // the copies first
       multiply<G, M, NI, NJ>(now, now + G::WCH, acc, wo, wr, m, g);
@@ -586,6 +649,7 @@ __global__ void __launch_bounds__(TN >= 256 ? 512 : 256) k_adapter_gemm(AdapterA
       wait_copies<(ST - 2) * G::kCopies>();
     else
       wait_copies<0>();
+    __builtin_amdgcn_s_barrier();
     if (c + ST - 1 < b1) stage(c + ST - 1, next);
     multiply<G, M, NI, NJ>(now, now + G::WCH, acc, wo, wr, m, g);
   };
@@ -604,7 +668,7 @@ __global__ void __launch_bounds__(TN >= 256 ? 512 : 256) k_adapter_gemm(AdapterA
 #pragma unroll
       for (int j = 0; j < NJ; ++j) out[(i * NJ + j) * 64] = acc[i][j];
   } else {
-    adapter_epilogue<T, TR, NI, NJ, 1>(a, acc, o0 + wo, pos0 + wr, n, m, g);
+    adapter_epilogue<T, TR, NI, NJ, kMaxParts>(a, acc, o0 + wo, pos0 + wr, n, m, g);
   }
 }
 
@@ -627,7 +691,7 @@ __global__ void __launch_bounds__(256) k_adapter_join(AdapterArgs a) {
   f32x4 acc[1][1] = {{in[0]}};
 #pragma unroll 8
   for (int h = 1; h < a.parts; ++h) acc[0][0] += in[(int64_t)h * (TN * TM / 4)];
-  adapter_epilogue<T, TR, 1, 1, kMaxDownParts>(a, acc, o0, pos0, n, lane & 15, lane >> 4);
+  adapter_epilogue<T, TR, 1, 1, kMaxJoinParts>(a, acc, o0, pos0, n, lane & 15, lane >> 4);
 }
 
 // The rows of each adapter in ascending order: rows[off[p] .. off[p + 1]), and
@@ -636,14 +700,36 @@ __global__ void __launch_bounds__(256) k_adapter_join(AdapterArgs a) {
 // take consecutive ranges of the rows.
 constexpr int kListWaves = 16;
 
+// b[p] [d][rank] as [rank][d], 64 rows at a time through LDS: the rank-wide
+// rows u then read b as t read a.
+template <typename T>
+__device__ __forceinline__ void adapter_flip(const AdapterArgs& a, int64_t item, T* bt) {
+  __shared__ T tile[64 * (NSC_MAX_RANK + 1)];
+  const int blocks = (a.d + 63) / 64;
+  const int64_t p = item / blocks;
+  const int d0 = (int)(item % blocks) * 64, nd = min(64, a.d - d0);
+  const T* from = static_cast<const T*>(a.b) + (p * a.d + d0) * a.rank;
+  for (int i = threadIdx.x; i < nd * a.rank; i += 64 * kListWaves)
+    tile[i / a.rank * (a.rank + 1) + i % a.rank] = from[i];
+  __syncthreads();
+  T* to = bt + p * a.rank * a.d + d0;
+  for (int i = threadIdx.x; i < 64 * a.rank; i += 64 * kListWaves) {
+    const int j = i / 64, r = i % 64;
+    if (r < nd) to[(int64_t)j * a.d + r] = tile[r * (a.rank + 1) + j];
+  }
+}
+
+template <typename T>
 __global__ void __launch_bounds__(64 * kListWaves) k_adapter_list(AdapterArgs a, int32_t* off,
-                                                                  int32_t* rows) {
+                                                                  int32_t* rows, int32_t listers,
+                                                                  T* bt) {
+  if ((int)blockIdx.x >= listers) return adapter_flip<T>(a, blockIdx.x - listers, bt);
   __shared__ int32_t less[kListWaves], same[kListWaves];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int64_t n = live_rows(a);
   const int64_t per = (n + kListWaves * 64 - 1) / (kListWaves * 64) * 64;
   const int64_t b = wave * per < n ? wave * per : n, e = b + per < n ? b + per : n;
-  for (int p = blockIdx.x; p <= a.n_adapters; p += gridDim.x) {
+  for (int p = blockIdx.x; p <= a.n_adapters; p += listers) {
     auto of = [&](int64_t r) {
       const int q = r < e ? a.ids[r] : -1;
       return q >= 0 && q < a.n_adapters ? q : (r < e ? a.n_adapters : INT_MAX);
@@ -679,7 +765,9 @@ __global__ void __launch_bounds__(64 * kListWaves) k_adapter_list(AdapterArgs a,
 // waves share them and add their sums through LDS; the other waves of a
 // workgroup take other columns.
 struct GradArgs {
-  const float* t[2];        // u, t
+  const float* t[2];        // u, t: [parts][max_rows][rp]
+  int32_t parts[2];
+  int64_t max_rows;
   const void* v[2];         // x, dy
   float* out[2];            // da, db
   int64_t v_stride[2];
@@ -700,7 +788,7 @@ __global__ void __launch_bounds__(512) k_adapter_grad(GradArgs a) {
   const int m = lane & 15, g = lane >> 4, rw = wave % RW;
   const int which = (int)blockIdx.x >= a.blocks0, p = blockIdx.y;
   const int blk = (int)blockIdx.x - (which ? a.blocks0 : 0);
-  const int cols = which ? a.cols[1] : a.cols[0];
+  const int cols = which ? a.cols[1] : a.cols[0], parts = which ? a.parts[1] : a.parts[0];
   const bool vec = (which ? a.vec[1] : a.vec[0]) != 0;
   const int64_t stride = which ? a.v_stride[1] : a.v_stride[0];
   const float* t = which ? a.t[1] : a.t[0];
@@ -727,7 +815,14 @@ __global__ void __launch_bounds__(512) k_adapter_grad(GradArgs a) {
         const T* x = v + (in ? row[s] : 0) * stride + c;
         xv[s] = vec ? load_frag<T, true>(x, in ? cols - c : 0)
                     : load_frag<T, false>(x, in ? cols - c : 0);
-        uv[s] = in ? t[(int64_t)(r + 4 * g + s) * a.rp + j0 + m] : 0.0f;
+        float part[kMaxParts];
+#pragma unroll
+        for (int h = 0; h < kMaxParts; ++h)
+          part[h] = in && (h == 0 || h < parts)
+                        ? t[(h * a.max_rows + r + 4 * g + s) * a.rp + j0 + m] : 0.0f;
+        uv[s] = 0.0f;
+#pragma unroll
+        for (int h = 0; h < kMaxParts; ++h) uv[s] += part[h];
       }
       next_rows(r + 16 * RW);
 #pragma unroll
@@ -819,14 +914,15 @@ size_t gemm_part_bytes(const GemmPlan& p, int64_t max_rows, int64_t outs) {
          p.parts * 4;
 }
 
-// Parts of the rank-wide rows' reduction beside a split product: about four
-// workgroups per CU, each wave of at least two steps of 64 bytes.
-int32_t down_parts(int64_t max_rows, int64_t len, int64_t es) {
-  const int64_t tiles = (max_rows + 15) / 16;
-  int64_t parts = tiles > 0 ? 4 * kNumCU / tiles : 1;
-  const int64_t most = len * es / (64 * 2 * kGemmDownWaves);
+// Parts of the rank-wide rows' reduction: about two workgroups per CU, four of
+// the smaller ones beside a split product, each wave of at least two chunks of
+// 128 bytes.
+int32_t down_parts(int64_t max_rows, int64_t len, int64_t es, bool split) {
+  const int64_t tiles = (max_rows + 15) / 16, per = split ? 4 : 2;
+  int64_t parts = tiles > 0 ? per * kNumCU / tiles : 1;
+  const int64_t most = len * es / (128 * 2 * (split ? kGemmDownWaves : kDownWaves));
   if (parts > most) parts = most;
-  if (parts > kMaxDownParts) parts = kMaxDownParts;
+  if (parts > (split ? kMaxJoinParts : kMaxParts)) parts = split ? kMaxJoinParts : kMaxParts;
   return parts < 1 ? 1 : (int32_t)parts;
 }
 
@@ -835,10 +931,10 @@ int32_t down_parts(int64_t max_rows, int64_t len, int64_t es) {
 constexpr int64_t kListRows = 256;
 
 // Workspace: the rank-wide rows t (backward: and u) by part, the product's
-// partial sums, and the rows by adapter.
+// partial sums, the rows by adapter, and backward b transposed.
 struct AdapterLayout {
-  size_t t, u, part, off, rows, total;
-  int32_t t_parts;
+  size_t t, u, part, off, rows, bt, total;
+  int32_t t_parts, u_parts;
   GemmPlan g;
   bool list;
 };
@@ -854,10 +950,14 @@ AdapterLayout adapter_layout(const nsc_adapter_desc& d, int64_t max_rows, bool b
   const int64_t es = type_bytes(d.dtype);
   const size_t rp = align_up(d.rank, 16);
   L.g = backward ? plan_gemm(max_rows, d.k, d.d, es) : plan_gemm(max_rows, d.d, d.k, es);
-  L.t_parts = backward || L.g.parts == 1 ? 1 : down_parts(max_rows, d.k, es);
+  L.t_parts = down_parts(max_rows, d.k, es, !backward && L.g.parts > 1);
+  L.u_parts = down_parts(max_rows, d.d, es, false);
   L.list = backward || max_rows >= kListRows;
   L.t = take((size_t)max_rows * rp * 4 * L.t_parts);
-  if (backward) L.u = take((size_t)max_rows * rp * 4);
+  if (backward) {
+    L.u = take((size_t)max_rows * rp * 4 * L.u_parts);
+    if (max_rows > 0) L.bt = take((size_t)d.n_adapters * d.rank * d.d * es);
+  }
   L.part = take(gemm_part_bytes(L.g, max_rows, backward ? d.k : d.d));
   if (L.list) {
     L.off = take(((size_t)d.n_adapters + 1) * 4);
@@ -880,16 +980,13 @@ int check_adapter_call(const nsc_adapter_desc* d, int64_t max_rows, const void* 
 }
 
 template <typename T>
-int launch_down(const AdapterArgs& a, bool vec, bool b, hipStream_t st) {
-  int64_t grid = (a.max_rows + 15) / 16;
+int launch_down(const DownArgs& d, int n, hipStream_t st) {
+  int64_t grid = (d.of[0].max_rows + 15) / 16;
   if (grid > 16 * kNumCU) grid = 16 * kNumCU;
-  const dim3 g((unsigned)grid), t(64 * kDownWaves);
-  if (b)
-    hipLaunchKernelGGL((k_adapter_down<T, false, true>), g, t, 0, st, a);
-  else if (vec)
-    hipLaunchKernelGGL((k_adapter_down<T, true, false>), g, t, 0, st, a);
-  else
-    hipLaunchKernelGGL((k_adapter_down<T, false, false>), g, t, 0, st, a);
+  int32_t parts = d.of[0].t_parts;
+  if (n > 1 && d.of[1].t_parts > parts) parts = d.of[1].t_parts;
+  hipLaunchKernelGGL(k_adapter_down<T>, dim3((unsigned)grid, (unsigned)parts, (unsigned)n),
+                     dim3(64 * kDownWaves), 0, st, d);
   NSC_CHECK_LAUNCH("k_adapter_down");
   return NSC_OK;
 }
@@ -950,10 +1047,16 @@ int launch_grad(GradArgs a, int32_t n_adapters, int64_t max_rows, hipStream_t st
   return NSC_OK;
 }
 
-int launch_list(AdapterArgs* a, int32_t* off, int32_t* rows, hipStream_t st) {
-  const int32_t most = 8 * kNumCU;
-  hipLaunchKernelGGL(k_adapter_list, dim3((unsigned)(a->n_adapters < most ? a->n_adapters + 1 : most)),
-                     dim3(64 * kListWaves), 0, st, *a, off, rows);
+// The rows by adapter, and (bt) b transposed.
+template <typename T>
+int launch_list(AdapterArgs* a, int32_t* off, int32_t* rows, T* bt, hipStream_t st) {
+  const int32_t most = 8 * kNumCU, listers = a->n_adapters < most ? a->n_adapters + 1 : most;
+  const int64_t flips = bt ? (int64_t)a->n_adapters * ((a->d + 63) / 64) : 0;
+  if (listers + flips > 0x7FFFFFFF)
+    return fail(NSC_E_SHAPE, "%d adapters of %d outputs are more than a launch holds",
+                a->n_adapters, a->d);
+  hipLaunchKernelGGL(k_adapter_list<T>, dim3((unsigned)(listers + flips)), dim3(64 * kListWaves), 0,
+                     st, *a, off, rows, listers, bt);
   NSC_CHECK_LAUNCH("k_adapter_list");
   a->rows = rows;
   return NSC_OK;
@@ -984,8 +1087,8 @@ int project(const nsc_adapter_desc& d, AdapterArgs a, unsigned char* ws, hipStre
   constexpr int E = 16 / sizeof(T);
   const AdapterLayout L = adapter_layout(d, a.max_rows, false);
   if (L.list)
-    if (int rc = launch_list(&a, reinterpret_cast<int32_t*>(ws + L.off),
-                             reinterpret_cast<int32_t*>(ws + L.rows), st))
+    if (int rc = launch_list<T>(&a, reinterpret_cast<int32_t*>(ws + L.off),
+                                reinterpret_cast<int32_t*>(ws + L.rows), nullptr, st))
       return rc;
   a.in_stride = d.x_stride;
   a.out_stride = d.y_stride;
@@ -998,8 +1101,11 @@ int project(const nsc_adapter_desc& d, AdapterArgs a, unsigned char* ws, hipStre
                    d.k % E == 0 && d.x_stride % E == 0;
   if (a.parts > 1) {
     a.down_blocks = (int32_t)((a.max_rows + 15) / 16) * a.t_parts;
-  } else if (int rc = launch_down<T>(a, vec, false, st)) {
-    return rc;
+  } else {
+    DownArgs t{};
+    t.of[0] = a;
+    t.vec[0] = vec;
+    if (int rc = launch_down<T>(t, 1, st)) return rc;
   }
   return launch_gemm<T, false>(a, L.g, vec, st);
 }
@@ -1013,20 +1119,25 @@ int backward(const nsc_adapter_desc& d, AdapterArgs a, const void* x, const void
   float* u = reinterpret_cast<float*>(ws + L.u);
   int32_t* off = reinterpret_cast<int32_t*>(ws + L.off);
   int32_t* rows = reinterpret_cast<int32_t*>(ws + L.rows);
-  if (int rc = launch_list(&a, off, rows, st)) return rc;
+  T* bt = a.max_rows > 0 ? reinterpret_cast<T*>(ws + L.bt) : nullptr;
+  if (int rc = launch_list<T>(&a, off, rows, bt, st)) return rc;
   if (a.max_rows > 0) {
-    a.x = x;
-    a.in_stride = d.x_stride;
-    a.t = t;
-    a.t_parts = 1;
-    if (int rc = launch_down<T>(
-            a, !misaligned(x, 16) && !misaligned(a.a, 16) && d.k % E == 0 && d.x_stride % E == 0,
-            false, st))
-      return rc;
+    DownArgs r{};
+    r.of[0] = a;  // t = scale x a^T
+    r.of[0].x = x;
+    r.of[0].in_stride = d.x_stride;
+    r.of[0].t = t;
+    r.of[0].t_parts = L.t_parts;
+    r.vec[0] = !misaligned(x, 16) && !misaligned(a.a, 16) && d.k % E == 0 && d.x_stride % E == 0;
     a.x = dy;
     a.in_stride = d.y_stride;
     a.t = u;
-    if (int rc = launch_down<T>(a, false, true, st)) return rc;
+    a.t_parts = L.u_parts;
+    r.of[1] = a;  // u = scale dy b
+    r.of[1].a = bt;
+    r.of[1].k = d.d;
+    r.vec[1] = !misaligned(dy, 16) && d.d % E == 0 && d.y_stride % E == 0;
+    if (int rc = launch_down<T>(r, 2, st)) return rc;
     if (dx) {
       a.out = dx;
       a.out_stride = d.x_stride;
@@ -1041,6 +1152,7 @@ int backward(const nsc_adapter_desc& d, AdapterArgs a, const void* x, const void
   GradArgs g{};
   g.off = off;
   g.rows = rows;
+  g.max_rows = a.max_rows;
   g.rank = a.rank;
   g.rp = a.rp;
   const void* v[2] = {x, dy};
@@ -1048,6 +1160,7 @@ int backward(const nsc_adapter_desc& d, AdapterArgs a, const void* x, const void
   const int32_t cols[2] = {d.k, d.d};
   for (int i = 0; i < 2; ++i) {
     g.t[i] = i ? t : u;
+    g.parts[i] = i ? L.t_parts : L.u_parts;
     g.v[i] = v[i];
     g.v_stride[i] = strides[i];
     g.cols[i] = cols[i];
