@@ -100,7 +100,7 @@ struct AdapterArgs {
   int32_t out4;             // four neighbouring outputs are one aligned store
   int64_t row_tiles;        // the product's grid: out_tiles x row_tiles x parts, after
   int32_t out_tiles;        // down_blocks workgroups of rank-wide rows
-  int32_t down_blocks;
+  int32_t down_blocks, down_sets;
 };
 
 __device__ __forceinline__ int64_t live_rows(const AdapterArgs& a) {
@@ -152,10 +152,11 @@ __device__ __forceinline__ int row_slot(int r, int c) { return c ^ (r & 7); }
 // lanes read 16 rows and a CU takes 7 bytes a cycle: 1,501 rows of 9,216 fp32
 // 85 us), adapter by adapter among the rows; a lane keeps the products of its
 // own row's adapter.  What is not whole aligned chunks is loaded as fragments.
+// Where rows of many adapters mix, `sets` workgroups share a tile's adapters.
 template <typename T, bool VEC, int W>
 __device__ __forceinline__ void adapter_down(const AdapterArgs& a, int64_t block, int64_t blocks,
-                                             int part, uint4* stage0, uint4* stage1, uint4* stage2,
-                                             f32x4 (*red)[64]) {
+                                             int part, int set, int sets, uint4* stage0,
+                                             uint4* stage1, uint4* stage2, f32x4 (*red)[64]) {
   using M = Mma<T>;
   constexpr int E = M::E, BK = 2 * M::KS;
   const int lane = threadIdx.x & 63;
@@ -170,9 +171,22 @@ __device__ __forceinline__ void adapter_down(const AdapterArgs& a, int64_t block
   const int s0 = (int)((int64_t)me * steps / parts), s1 = (int)((int64_t)(me + 1) * steps / parts);
   const int cr = lane >> 3, cs = row_slot(cr, lane & 7) * E;  // a copy's row (and + 8), values
   for (int64_t pos0 = block * 16; pos0 < n; pos0 += blocks * 16) {
-    const bool in = pos0 + m < n;
+    bool in = pos0 + m < n;
     const int64_t row = row_at(a, in ? pos0 + m : n - 1);
-    const int mine = in ? adapter_of(a, row) : INT_MAX;
+    int mine = in ? adapter_of(a, row) : INT_MAX;
+    if (sets > 1) {  // every sets-th of the rows' adapters; without one: set 0
+      int at = 0, of = 0;
+      for (uint32_t t = with_adapter(mine); t; at = at + 1 == sets ? 0 : at + 1) {
+        const int p = pick_adapter(mine, t);
+        t &= ~rows_of(mine, p);
+        if (mine == p) of = at;
+      }
+      if (__ballot(in && of == set) == 0) continue;
+      if (of != set) {
+        in = false;
+        mine = INT_MAX;
+      }
+    }
     const float scale = mine != INT_MAX ? a.scale[mine] : 0.0f;
     const uint32_t some = with_adapter(mine);
     const T* x = static_cast<const T*>(a.x) + row * a.in_stride;
@@ -280,10 +294,10 @@ __global__ void __launch_bounds__(64 * kDownWaves) k_adapter_down(DownArgs d) {
   const AdapterArgs& a = blockIdx.z ? d.of[1] : d.of[0];
   if ((int)blockIdx.y >= a.t_parts) return;
   if (blockIdx.z ? d.vec[1] : d.vec[0])
-    adapter_down<T, true, kDownWaves>(a, blockIdx.x, gridDim.x, blockIdx.y, stage0, stage1, stage2,
-                                      red);
+    adapter_down<T, true, kDownWaves>(a, blockIdx.x, gridDim.x, blockIdx.y, 0, 1, stage0, stage1,
+                                      stage2, red);
   else
-    adapter_down<T, false, kDownWaves>(a, blockIdx.x, gridDim.x, blockIdx.y, stage0, stage1,
+    adapter_down<T, false, kDownWaves>(a, blockIdx.x, gridDim.x, blockIdx.y, 0, 1, stage0, stage1,
                                        stage2, red);
 }
 
@@ -351,20 +365,27 @@ struct Gemm {
   }
 };
 
-// Adds the rank-wide rows' products and the bias to outputs o0 .. of positions
-// pos0 .. and stores them.  TP: most parts of the rank-wide rows.
-template <typename T, bool TR, int NI, int NJ, int TP>
-__device__ __forceinline__ void adapter_epilogue(const AdapterArgs& a, f32x4 (&acc)[NI][NJ],
-                                                 int o0, int64_t pos0, int64_t n, int m, int g) {
-  const int outs = TR ? a.k : a.d;
+// The rows at 16 NJ positions and their adapters.
+template <int NJ>
+struct TileRows {
   int64_t row[NJ];
   int mine[NJ];
+  __device__ __forceinline__ TileRows(const AdapterArgs& a, int64_t pos0, int64_t n, int m) {
 #pragma unroll
-  for (int j = 0; j < NJ; ++j) {
-    const int64_t pos = pos0 + j * 16 + m;
-    row[j] = pos < n ? row_at(a, pos) : 0;
-    mine[j] = pos < n ? adapter_of(a, row[j]) : INT_MAX;
+    for (int j = 0; j < NJ; ++j) {
+      const int64_t pos = pos0 + j * 16 + m;
+      row[j] = pos < n ? row_at(a, pos) : 0;
+      mine[j] = pos < n ? adapter_of(a, row[j]) : INT_MAX;
+    }
   }
+};
+
+// Adds the rank-wide rows' products to outputs o0 .. of positions pos0 .. .
+template <typename T, bool TR, int NI, int NJ>
+__device__ __forceinline__ void add_ranks(const AdapterArgs& a, f32x4 (&acc)[NI][NJ],
+                                          const int (&mine)[NJ], int o0, int64_t pos0, int m,
+                                          int g) {
+  const int outs = TR ? a.k : a.d;
   for (int q0 = 0; q0 < a.rp; q0 += 16) {
     const int q = q0 + 4 * g;
     f32x4 tv[NJ];
@@ -374,21 +395,18 @@ __device__ __forceinline__ void adapter_epilogue(const AdapterArgs& a, f32x4 (&a
       tv[j] = f32x4{0.f, 0.f, 0.f, 0.f};
       todo[j] = with_adapter(mine[j]);
       if (mine[j] != INT_MAX) {
-        f32x4 v[TP];
+        f32x4 v[kMaxParts];
 #pragma unroll
-        for (int h = 0; h < TP; ++h) {
+        for (int h = 0; h < kMaxParts; ++h) {
           v[h] = f32x4{0.f, 0.f, 0.f, 0.f};
           if (h == 0 || h < a.t_parts)
             v[h] = *reinterpret_cast<const f32x4*>(
                 a.t + (h * a.max_rows + pos0 + j * 16 + m) * a.rp + q);
         }
 #pragma unroll
-        for (int h = 0; h < TP; ++h) tv[j] += v[h];
+        for (int h = 0; h < kMaxParts; ++h) tv[j] += v[h];
       }
     }
-    // PB adapters at a time, whose loads are under way together: a join's waves
-    // have one block each and wait for little else
-    constexpr int PB = NI * NJ == 1 ? 4 : 1;
     auto load_b = [&](int p, f32x4 (&bv)[NI]) __attribute__((always_inline)) {
 #pragma unroll
       for (int i = 0; i < NI; ++i) {
@@ -439,21 +457,76 @@ __device__ __forceinline__ void adapter_epilogue(const AdapterArgs& a, f32x4 (&a
       return p;
     };
     for (int p = next(); p != INT_MAX; p = next()) {
-      f32x4 bv[PB][NI];
-      int ps[PB];
-      ps[0] = p;
-      load_b(p, bv[0]);
-#pragma unroll
-      for (int k = 1; k < PB; ++k) {
-        ps[k] = next();
-        if (ps[k] != INT_MAX) load_b(ps[k], bv[k]);
-      }
-      add_b(p, bv[0]);
-#pragma unroll
-      for (int k = 1; k < PB; ++k)
-        if (ps[k] != INT_MAX) add_b(ps[k], bv[k]);
+      f32x4 bv[NI];
+      load_b(p, bv);
+      add_b(p, bv);
     }
   }
+}
+
+// The rank-wide row's products of four neighbouring outputs of one position by
+// a lane alone, with its adapter's own values: no adapter waits for another
+// one's loads.
+template <typename T, bool TR>
+__device__ __forceinline__ void row_ranks(const AdapterArgs& a, f32x4& acc, int p, int o,
+                                          int64_t pos) {
+  const int outs = TR ? a.k : a.d;
+  for (int q0 = 0; q0 < a.rank; q0 += 8) {
+    f32x4 t[2] = {}, tp[kMaxJoinParts][2];
+#pragma unroll
+    for (int h = 0; h < kMaxJoinParts; ++h)
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+        tp[h][i] = h < a.t_parts ? *reinterpret_cast<const f32x4*>(
+                                       a.t + (h * a.max_rows + pos) * a.rp + q0 + 4 * i)
+                                 : f32x4{0.f, 0.f, 0.f, 0.f};
+    f32x4 b[4][2];  // TR: of rank values q0 + 2 e + i (outputs o ..); else of output o + e
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        if constexpr (TR) {
+          const int q = q0 + 2 * e + i;
+          const T* at = static_cast<const T*>(a.a) + ((int64_t)p * a.rank + q) * a.k + o;
+          b[e][i] = load4(at, q < a.rank ? outs - o : 0);
+        } else {
+          const int q = q0 + 4 * i, oe = o + e < outs ? o + e : outs - 1;
+          const T* at = static_cast<const T*>(a.b) + ((int64_t)p * a.d + oe) * a.rank + q;
+          if (a.b4) {
+            b[e][i] = f32x4{0.f, 0.f, 0.f, 0.f};
+            if (q < a.rank) {
+              const Vec<T, 4> v = *reinterpret_cast<const Vec<T, 4>*>(at);
+              b[e][i] = f32x4{(float)v.e[0], (float)v.e[1], (float)v.e[2], (float)v.e[3]};
+            }
+          } else {
+            b[e][i] = load4(at, a.rank - q);
+          }
+        }
+      }
+#pragma unroll
+    for (int h = 0; h < kMaxJoinParts; ++h)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) t[i] += tp[h][i];
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        if constexpr (TR) {
+          acc += t[(2 * e + i) / 4][(2 * e + i) % 4] * b[e][i];
+        } else {
+#pragma unroll
+          for (int k = 0; k < 4; ++k) acc[e] = fmaf(t[i][k], b[e][i][k], acc[e]);
+        }
+      }
+  }
+}
+
+// Adds the bias to outputs o0 .. of positions pos0 .. and stores them.
+template <typename T, bool TR, int NI, int NJ>
+__device__ __forceinline__ void store_outputs(const AdapterArgs& a, const f32x4 (&acc)[NI][NJ],
+                                              const int64_t (&row)[NJ], int o0, int64_t pos0,
+                                              int64_t n, int m, int g) {
+  const int outs = TR ? a.k : a.d;
   f32x4 bias[NI];
 #pragma unroll
   for (int i = 0; i < NI; ++i)
@@ -527,9 +600,11 @@ __global__ void __launch_bounds__(TN >= 256 ? 512 : 256) k_adapter_gemm(AdapterA
   if constexpr (!TR && TN < 256) {  // a call whose product is split takes its rank-wide rows here
     if (block < a.down_blocks) {
       static_assert(kStage >= kGemmDownWaves * 256 && kGemmDownWaves * 64 == TH, "in the stages");
-      adapter_down<T, VEC, kGemmDownWaves>(a, block / a.t_parts, a.down_blocks / a.t_parts,
-                                           (int)(block % a.t_parts), stage0, stage1, stage2,
-                                           reinterpret_cast<f32x4(*)[64]>(stage0));
+      const int per = a.t_parts * a.down_sets;
+      adapter_down<T, VEC, kGemmDownWaves>(
+          a, block / per, a.down_blocks / per, (int)(block % a.t_parts),
+          (int)(block % per / a.t_parts), a.down_sets, stage0, stage1, stage2,
+          reinterpret_cast<f32x4(*)[64]>(stage0));
       return;
     }
     block -= a.down_blocks;
@@ -668,12 +743,15 @@ __global__ void __launch_bounds__(TN >= 256 ? 512 : 256) k_adapter_gemm(AdapterA
 #pragma unroll
       for (int j = 0; j < NJ; ++j) out[(i * NJ + j) * 64] = acc[i][j];
   } else {
-    adapter_epilogue<T, TR, NI, NJ, kMaxParts>(a, acc, o0 + wo, pos0 + wr, n, m, g);
+    const TileRows<NJ> rows(a, pos0 + wr, n, m);
+    add_ranks<T, TR, NI, NJ>(a, acc, rows.mine, o0 + wo, pos0 + wr, m, g);
+    store_outputs<T, TR>(a, acc, rows.row, o0 + wo, pos0 + wr, n, m, g);
   }
 }
 
 // Adds a tile's parts in order, then its epilogue: a wave per 16 outputs of 16
-// rows.
+// rows.  The rows' adapters are loaded first and everything else at once after
+// them: the kernel's time is its chain of loads.
 template <typename T, bool TR, int TN, int TM>
 __global__ void __launch_bounds__(256) k_adapter_join(AdapterArgs a) {
   using G = Gemm<T, TR, TN, TM>;
@@ -688,10 +766,29 @@ __global__ void __launch_bounds__(256) k_adapter_join(AdapterArgs a) {
   if (pos0 >= n || o0 >= (TR ? a.k : a.d)) return;
   const f32x4* in =
       reinterpret_cast<const f32x4*>(a.part) + tile * a.parts * (TN * TM / 4) + f * 64 + lane;
-  f32x4 acc[1][1] = {{in[0]}};
-#pragma unroll 8
-  for (int h = 1; h < a.parts; ++h) acc[0][0] += in[(int64_t)h * (TN * TM / 4)];
-  adapter_epilogue<T, TR, 1, 1, kMaxJoinParts>(a, acc, o0, pos0, n, lane & 15, lane >> 4);
+  const int m = lane & 15, g = lane >> 4;
+  const TileRows<1> rows(a, pos0, n, m);
+  constexpr int P = 8;  // parts whose loads are under way while the adapters' are
+  f32x4 part[P];
+#pragma unroll
+  for (int h = 0; h < P; ++h)
+    part[h] = h < a.parts ? in[(int64_t)h * (TN * TM / 4)] : f32x4{0.f, 0.f, 0.f, 0.f};
+  f32x4 acc[1][1] = {{f32x4{0.f, 0.f, 0.f, 0.f}}};
+  if (rows.mine[0] != INT_MAX)
+    row_ranks<T, TR>(a, acc[0][0], rows.mine[0], o0 + 4 * g, pos0 + m);
+  f32x4 sum = part[0];
+#pragma unroll
+  for (int h = 1; h < P; ++h) sum += part[h];
+  for (int h0 = P; h0 < a.parts; h0 += P) {
+#pragma unroll
+    for (int h = 0; h < P; ++h)
+      part[h] = h0 + h < a.parts ? in[(int64_t)(h0 + h) * (TN * TM / 4)]
+                                 : f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int h = 0; h < P; ++h) sum += part[h];
+  }
+  acc[0][0] += sum;
+  store_outputs<T, TR>(a, acc, rows.row, o0, pos0, n, m, g);
 }
 
 // The rows of each adapter in ascending order: rows[off[p] .. off[p + 1]), and
@@ -805,34 +902,42 @@ __global__ void __launch_bounds__(512) k_adapter_grad(GradArgs a) {
 #pragma unroll
       for (int s = 0; s < 4; ++s) row[s] = r + 4 * g + s < e ? a.rows[r + 4 * g + s] : -1;
     };
-    next_rows(b + rw * 16);
-    for (int32_t r = b + rw * 16; r < e; r += 16 * RW) {
-      f32x4 uv;
-      uint4 xv[4];
+    auto all_rows = [&](auto one) __attribute__((always_inline)) {  // one part of t, or more
+      next_rows(b + rw * 16);
+      for (int32_t r = b + rw * 16; r < e; r += 16 * RW) {
+        f32x4 uv;
+        uint4 xv[4];
 #pragma unroll
-      for (int s = 0; s < 4; ++s) {
-        const bool in = row[s] >= 0;
-        const T* x = v + (in ? row[s] : 0) * stride + c;
-        xv[s] = vec ? load_frag<T, true>(x, in ? cols - c : 0)
-                    : load_frag<T, false>(x, in ? cols - c : 0);
-        float part[kMaxParts];
+        for (int s = 0; s < 4; ++s) {
+          const bool in = row[s] >= 0;
+          const T* x = v + (in ? row[s] : 0) * stride + c;
+          xv[s] = vec ? load_frag<T, true>(x, in ? cols - c : 0)
+                      : load_frag<T, false>(x, in ? cols - c : 0);
+          const float* ts = t + (int64_t)(r + 4 * g + s) * a.rp + j0 + m;
+          uv[s] = in ? *ts : 0.0f;
+          if constexpr (!decltype(one)::value) {
+            float part[kMaxParts - 1];
 #pragma unroll
-        for (int h = 0; h < kMaxParts; ++h)
-          part[h] = in && (h == 0 || h < parts)
-                        ? t[(h * a.max_rows + r + 4 * g + s) * a.rp + j0 + m] : 0.0f;
-        uv[s] = 0.0f;
+            for (int h = 1; h < kMaxParts; ++h)
+              part[h - 1] = in && h < parts ? ts[h * a.max_rows * a.rp] : 0.0f;
 #pragma unroll
-        for (int h = 0; h < kMaxParts; ++h) uv[s] += part[h];
+            for (int h = 1; h < kMaxParts; ++h) uv[s] += part[h - 1];
+          }
+        }
+        next_rows(r + 16 * RW);
+#pragma unroll
+        for (int i = 0; i < CPL; ++i) {
+          f32x4 xi;
+#pragma unroll
+          for (int s = 0; s < 4; ++s) xi[s] = (float)__builtin_bit_cast(Vec<T, CPL>, xv[s]).e[i];
+          acc[i] = mma_f32(uv, xi, acc[i]);
+        }
       }
-      next_rows(r + 16 * RW);
-#pragma unroll
-      for (int i = 0; i < CPL; ++i) {
-        f32x4 xi;
-#pragma unroll
-        for (int s = 0; s < 4; ++s) xi[s] = (float)__builtin_bit_cast(Vec<T, CPL>, xv[s]).e[i];
-        acc[i] = mma_f32(uv, xi, acc[i]);
-      }
-    }
+    };
+    if (parts == 1)
+      all_rows(std::true_type{});
+    else
+      all_rows(std::false_type{});
     if constexpr (RW > 1) {
       __syncthreads();  // red is read before it is written again
 #pragma unroll
@@ -896,12 +1001,13 @@ GemmPlan plan_gemm(int64_t max_rows, int64_t outs, int64_t len, int64_t es) {
   auto tiles = [&](int64_t tn, int64_t tm) {
     return (outs + tn - 1) / tn * ((max_rows + tm - 1) / tm);
   };
-  const bool big = tiles(256, 128) >= kNumCU;
+  const int64_t blocks = (len * es + 127) / 128;
+  const bool big = tiles(256, 128) >= kNumCU && blocks >= 16;
   p.tn = big ? 256 : 128;
   p.tm = big ? 128 : max_rows <= 16 ? 16 : 64;
-  const int64_t t = tiles(p.tn, p.tm), blocks = (len * es + 127) / 128;
-  // parts for about two workgroups per CU, each of at least four blocks
-  int64_t parts = t > 0 && t < kNumCU ? 2 * kNumCU / t : 1;
+  const int64_t t = tiles(p.tn, p.tm);
+  // parts for about a workgroup per CU, each of at least four blocks
+  int64_t parts = t > 0 ? kNumCU / t : 1;
   if (parts > blocks / 4) parts = blocks / 4;
   if (parts > 64) parts = 64;
   p.parts = parts < 1 ? 1 : (int32_t)parts;
@@ -1100,7 +1206,10 @@ int project(const nsc_adapter_desc& d, AdapterArgs a, unsigned char* ws, hipStre
   const bool vec = !misaligned(a.x, 16) && !misaligned(a.a, 16) && !misaligned(a.w, 16) &&
                    d.k % E == 0 && d.x_stride % E == 0;
   if (a.parts > 1) {
-    a.down_blocks = (int32_t)((a.max_rows + 15) / 16) * a.t_parts;
+    // few tiles: several workgroups share the adapters of each
+    const int32_t tiles = (int32_t)((a.max_rows + 15) / 16) * a.t_parts;
+    a.down_sets = tiles * 8 <= kNumCU ? 8 : tiles * 2 <= kNumCU ? kNumCU / tiles : 1;
+    a.down_blocks = tiles * a.down_sets;
   } else {
     DownArgs t{};
     t.of[0] = a;
