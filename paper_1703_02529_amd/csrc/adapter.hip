@@ -30,14 +30,20 @@ typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 // sides.)
 template <typename T> struct Mma;
 template <> struct Mma<__bf16> {
-  static constexpr int E = 8, KS = 32;
+  static constexpr int E = 8, KS = 32, kParts = 1;
+  static __device__ __forceinline__ f32x4 part(uint4 a, uint4 b, f32x4 c, int) {
+    return mma(a, b, c);
+  }
   static __device__ __forceinline__ f32x4 mma(uint4 a, uint4 b, f32x4 c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a),
                                                    __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
   }
 };
 template <> struct Mma<_Float16> {
-  static constexpr int E = 8, KS = 32;
+  static constexpr int E = 8, KS = 32, kParts = 1;
+  static __device__ __forceinline__ f32x4 part(uint4 a, uint4 b, f32x4 c, int) {
+    return mma(a, b, c);
+  }
   static __device__ __forceinline__ f32x4 mma(uint4 a, uint4 b, f32x4 c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a),
                                                   __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
@@ -49,7 +55,11 @@ __device__ __forceinline__ f32x4 mma_f32(const f32x4& a, const f32x4& b, f32x4 c
   return c;
 }
 template <> struct Mma<float> {
-  static constexpr int E = 4, KS = 16;
+  static constexpr int E = 4, KS = 16, kParts = 4;
+  static __device__ __forceinline__ f32x4 part(uint4 a, uint4 b, f32x4 c, int e) {
+    return __builtin_amdgcn_mfma_f32_16x16x4f32(__builtin_bit_cast(f32x4, a)[e],
+                                                __builtin_bit_cast(f32x4, b)[e], c, 0, 0, 0);
+  }
   static __device__ __forceinline__ f32x4 mma(uint4 a, uint4 b, f32x4 c) {
     return mma_f32(__builtin_bit_cast(f32x4, a), __builtin_bit_cast(f32x4, b), c);
   }
@@ -323,7 +333,7 @@ struct Gemm {
   static constexpr int NI = TN / WN / 16, NJ = TM / WM / 16;
   static constexpr int WCH = TN * BK * sizeof(T) / 16, XCH = TM * 8;  // 16-byte chunks of a tile
   static constexpr int RCH = TR ? TN / E : 8;         // chunks of a row of the weights' tile
-  static constexpr int kStages = TM >= 64 ? 3 : 4;
+  static constexpr int kStages = TM >= 64 ? (TR && TN < 256 ? 2 : 3) : 4;
   // copies per thread and block, at least (a wave's outstanding ones of a whole block)
   static constexpr int kCopies = WCH / kThreads + XCH / kThreads;
 
@@ -569,10 +579,14 @@ __device__ __forceinline__ void multiply(const uint4* wl, const uint4* xl, f32x4
       const int r = wr + j * 16 + m;
       bv[j] = xl[r * 8 + G::xslot(r, 4 * s + g)];
     }
+    // (of the four fp32 products of a step, one of every block before the next:
+    // none waits for the one before it)
 #pragma unroll
-    for (int i = 0; i < NI; ++i)
+    for (int e = 0; e < M::kParts; ++e)
 #pragma unroll
-      for (int j = 0; j < NJ; ++j) acc[i][j] = M::mma(av[i], bv[j], acc[i][j]);
+      for (int i = 0; i < NI; ++i)
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) acc[i][j] = M::part(av[i], bv[j], acc[i][j], e);
   }
 }
 
@@ -595,7 +609,9 @@ __global__ void __launch_bounds__(TN >= 256 ? 512 : 256) k_adapter_gemm(AdapterA
   // compiler takes every read to need all the copies under way and waits for
   // them before it.
   constexpr int kStage = G::WCH + G::XCH;
-  __shared__ uint4 stage0[kStage], stage1[kStage], stage2[kStage], stage3[ST > 3 ? kStage : 1];
+  __shared__ uint4 stage0[kStage], stage1[kStage], stage2[ST > 2 ? kStage : 1];
+  __shared__ uint4 stage3[ST > 3 ? kStage : 1];
+  uint4* const last = ST > 3 ? stage3 : ST > 2 ? stage2 : stage1;
   int64_t block = blockIdx.x;
   if constexpr (!TR && TN < 256) {  // a call whose product is split takes its rank-wide rows here
     if (block < a.down_blocks) {
@@ -704,17 +720,17 @@ __global__ void __launch_bounds__(TN >= 256 ? 512 : 256) k_adapter_gemm(AdapterA
       multiply<G, M, NI, NJ>(now, now + G::WCH, acc, wo, wr, m, g);
     };
     copy(b0, stage0);
-    copy(b0 + 1, stage1);
+    if constexpr (ST > 2) copy(b0 + 1, stage1);
     if constexpr (ST > 3) copy(b0 + 2, stage2);
     for (; b + 2 * ST - 1 <= bw; b += ST) {
-      step(b, stage0, ST > 3 ? stage3 : stage2);
+      step(b, stage0, last);
       step(b + 1, stage1, stage0);
-      step(b + 2, stage2, stage1);
+      if constexpr (ST > 2) step(b + 2, stage2, stage1);
       if constexpr (ST > 3) step(b + 3, stage3, stage2);
     }
   } else {
     if (b0 < b1) stage(b0, stage0);
-    if (b0 + 1 < b1) stage(b0 + 1, stage1);
+    if (ST > 2 && b0 + 1 < b1) stage(b0 + 1, stage1);
     if (ST > 3 && b0 + 2 < b1) stage(b0 + 2, stage2);
   }
   // The last blocks, and short reductions: as above, each block as it may be
@@ -729,9 +745,9 @@ __global__ void __launch_bounds__(TN >= 256 ? 512 : 256) k_adapter_gemm(AdapterA
     multiply<G, M, NI, NJ>(now, now + G::WCH, acc, wo, wr, m, g);
   };
   for (; b < b1; b += ST) {
-    step(b, stage0, ST > 3 ? stage3 : stage2);
+    step(b, stage0, last);
     if (b + 1 < b1) step(b + 1, stage1, stage0);
-    if (b + 2 < b1) step(b + 2, stage2, stage1);
+    if (ST > 2 && b + 2 < b1) step(b + 2, stage2, stage1);
     if (ST > 3 && b + 3 < b1) step(b + 3, stage3, stage2);
   }
   if (a.parts > 1) {
