@@ -479,21 +479,35 @@ def make_adapter_desc(k, d, rank, n_adapters, dtype=NSC_T_F32, x_stride=None,
                        d if y_stride is None else y_stride)
 
 
-def _layer_ptrs(stream, *tensors):
-    """The tensors' pointers; all of them must be on the stream's device and
-    that device the current one (the library launches there)."""
+def _layer_args(stream, *tensors):
+    """The tensors' pointers and the stream's handle; all of them must be on the
+    stream's device and that device the current one (the library launches there)."""
     import torch
     s = stream if stream is not None else torch.cuda.current_stream()
+    dev = s.device_index
+    if dev != torch.cuda.current_device():
+        raise ValueError(f"the stream's device {dev} is not the current one")
+    out = []
     for t in tensors:
-        if t is not None and t.is_cuda and t.device != s.device:
-            raise ValueError(f"tensor on {t.device}, stream on {s.device}")
-    if s.device.index != torch.cuda.current_device():
-        raise ValueError(f"the stream's device {s.device} is not the current one")
-    return [_ptr(t) for t in tensors]
+        if t is None:
+            out.append(None)
+            continue
+        if t.get_device() != dev:
+            raise ValueError(f"device tensor on device {dev} expected, got one on {t.device}")
+        if not t.is_contiguous():
+            raise ValueError("contiguous tensor expected")
+        out.append(t.data_ptr())
+    out.append(s.cuda_stream)
+    return out
+
+
+def _nbytes(t):
+    return t.numel() * t.element_size() if t is not None else 0
 
 
 def _hold(what, t, dtype, numel):
-    """t must hold `numel` elements of the type: the library sees only its pointer."""
+    """t must hold `numel` elements of the type: the library sees only its
+    pointer."""
     if t is not None and (t.dtype != dtype or t.numel() < numel):
         raise ValueError(f"{what}: {numel} elements of {dtype} expected, got {t.numel()} of "
                          f"{t.dtype}")
@@ -501,7 +515,9 @@ def _hold(what, t, dtype, numel):
 
 def _elem(dtype):
     import torch
-    return {NSC_T_F32: torch.float32, NSC_T_BF16: torch.bfloat16, NSC_T_F16: torch.float16}[dtype]
+    if dtype == NSC_T_BF16:
+        return torch.bfloat16
+    return torch.float16 if dtype == NSC_T_F16 else torch.float32
 
 
 def _span(n, stride, width):
@@ -523,36 +539,41 @@ def nsc_group_norm_workspace_bytes(desc: NormDesc, max_count: int, backward: boo
 def nsc_group_norm(desc: NormDesc, x, gamma, beta, y, ws, max_count, stats=None, count=None,
                    stream=None):
     import torch
-    _check(nsc_norm_check(desc), "nsc_group_norm")
     t, e = _elem(desc.dtype), desc.h * desc.w * desc.c
-    _hold("x", x, t, _span(max_count, desc.x_stride, e))
-    _hold("y", y, t, _span(max_count, desc.y_stride, e))
-    _hold("gamma", gamma, torch.float32, desc.c)
-    _hold("beta", beta, torch.float32, desc.c)
-    _hold("stats", stats, torch.float32, 2 * max_count * desc.groups)
-    _hold("count", count, torch.int32, 1)
-    x, gamma, beta, count, y, stats, w = _layer_ptrs(stream, x, gamma, beta, count, y, stats, ws)
+    try:
+        _hold("x", x, t, _span(max_count, desc.x_stride, e))
+        _hold("y", y, t, _span(max_count, desc.y_stride, e))
+        _hold("gamma", gamma, torch.float32, desc.c)
+        _hold("beta", beta, torch.float32, desc.c)
+        _hold("stats", stats, torch.float32, 2 * max_count * desc.groups)
+        _hold("count", count, torch.int32, 1)
+    except ValueError:
+        _check(nsc_norm_check(desc), "nsc_group_norm")  # a bad description comes first
+        raise
+    x, gamma, beta, count, y, stats, w, st = _layer_args(stream, x, gamma, beta, count, y, stats,
+                                                         ws)
     _check(lib().nsc_group_norm(ctypes.byref(desc), x, gamma, beta, count, max_count, y, stats, w,
-                                ws.numel() * ws.element_size() if ws is not None else 0,
-                                _stream(stream)), "nsc_group_norm")
+                                _nbytes(ws), st), "nsc_group_norm")
 
 
 def nsc_group_norm_backward(desc: NormDesc, x, dy, gamma, beta, stats, dx, dgamma, dbeta, ws,
                             max_count, count=None, stream=None):
     import torch
-    _check(nsc_norm_check(desc), "nsc_group_norm_backward")
     t, e = _elem(desc.dtype), desc.h * desc.w * desc.c
-    for what, v, stride in (("x", x, desc.x_stride), ("dx", dx, desc.x_stride),
-                            ("dy", dy, desc.y_stride)):
-        _hold(what, v, t, _span(max_count, stride, e))
-    for what, v in (("gamma", gamma), ("beta", beta), ("dgamma", dgamma), ("dbeta", dbeta)):
-        _hold(what, v, torch.float32, desc.c)
-    _hold("stats", stats, torch.float32, 2 * max_count * desc.groups)
-    _hold("count", count, torch.int32, 1)
-    p = _layer_ptrs(stream, x, dy, gamma, beta, stats, count, dx, dgamma, dbeta, ws)
-    _check(lib().nsc_group_norm_backward(ctypes.byref(desc), *p[:6], max_count, *p[6:],
-                                         ws.numel() * ws.element_size() if ws is not None else 0,
-                                         _stream(stream)), "nsc_group_norm_backward")
+    try:
+        for what, v, stride in (("x", x, desc.x_stride), ("dx", dx, desc.x_stride),
+                                ("dy", dy, desc.y_stride)):
+            _hold(what, v, t, _span(max_count, stride, e))
+        for what, v in (("gamma", gamma), ("beta", beta), ("dgamma", dgamma), ("dbeta", dbeta)):
+            _hold(what, v, torch.float32, desc.c)
+        _hold("stats", stats, torch.float32, 2 * max_count * desc.groups)
+        _hold("count", count, torch.int32, 1)
+    except ValueError:
+        _check(nsc_norm_check(desc), "nsc_group_norm_backward")  # a bad description comes first
+        raise
+    p = _layer_args(stream, x, dy, gamma, beta, stats, count, dx, dgamma, dbeta, ws)
+    _check(lib().nsc_group_norm_backward(ctypes.byref(desc), *p[:6], max_count, *p[6:-1],
+                                         _nbytes(ws), p[-1]), "nsc_group_norm_backward")
 
 
 def nsc_adapter_check(desc: AdapterDesc) -> int:
@@ -580,30 +601,34 @@ def _hold_adapters(desc, w, a, b, scale, ids, count, max_rows):
 def nsc_adapter_project(desc: AdapterDesc, x, w, bias, a, b, scale, ids, y, ws, max_rows,
                         count=None, stream=None):
     import torch
-    _check(nsc_adapter_check(desc), "nsc_adapter_project")
     t = _elem(desc.dtype)
-    _hold("x", x, t, _span(max_rows, desc.x_stride, desc.k))
-    _hold("y", y, t, _span(max_rows, desc.y_stride, desc.d))
-    _hold("bias", bias, torch.float32, desc.d)
-    _hold_adapters(desc, w, a, b, scale, ids, count, max_rows)
-    p = _layer_ptrs(stream, x, w, bias, a, b, scale, ids, count, y, ws)
-    _check(lib().nsc_adapter_project(ctypes.byref(desc), *p[:8], max_rows, *p[8:],
-                                     ws.numel() * ws.element_size() if ws is not None else 0,
-                                     _stream(stream)), "nsc_adapter_project")
+    try:
+        _hold("x", x, t, _span(max_rows, desc.x_stride, desc.k))
+        _hold("y", y, t, _span(max_rows, desc.y_stride, desc.d))
+        _hold("bias", bias, torch.float32, desc.d)
+        _hold_adapters(desc, w, a, b, scale, ids, count, max_rows)
+    except ValueError:
+        _check(nsc_adapter_check(desc), "nsc_adapter_project")  # a bad description comes first
+        raise
+    p = _layer_args(stream, x, w, bias, a, b, scale, ids, count, y, ws)
+    _check(lib().nsc_adapter_project(ctypes.byref(desc), *p[:8], max_rows, *p[8:-1], _nbytes(ws),
+                                     p[-1]), "nsc_adapter_project")
 
 
 def nsc_adapter_backward(desc: AdapterDesc, x, dy, w, a, b, scale, ids, dx, da, db, ws, max_rows,
                          count=None, stream=None):
     import torch
-    _check(nsc_adapter_check(desc), "nsc_adapter_backward")
     t = _elem(desc.dtype)
-    _hold("x", x, t, _span(max_rows, desc.x_stride, desc.k))
-    _hold("dx", dx, t, _span(max_rows, desc.x_stride, desc.k))
-    _hold("dy", dy, t, _span(max_rows, desc.y_stride, desc.d))
-    _hold("da", da, torch.float32, desc.n_adapters * desc.rank * desc.k)
-    _hold("db", db, torch.float32, desc.n_adapters * desc.rank * desc.d)
-    _hold_adapters(desc, w, a, b, scale, ids, count, max_rows)
-    p = _layer_ptrs(stream, x, dy, w, a, b, scale, ids, count, dx, da, db, ws)
-    _check(lib().nsc_adapter_backward(ctypes.byref(desc), *p[:8], max_rows, *p[8:],
-                                      ws.numel() * ws.element_size() if ws is not None else 0,
-                                      _stream(stream)), "nsc_adapter_backward")
+    try:
+        _hold("x", x, t, _span(max_rows, desc.x_stride, desc.k))
+        _hold("dx", dx, t, _span(max_rows, desc.x_stride, desc.k))
+        _hold("dy", dy, t, _span(max_rows, desc.y_stride, desc.d))
+        _hold("da", da, torch.float32, desc.n_adapters * desc.rank * desc.k)
+        _hold("db", db, torch.float32, desc.n_adapters * desc.rank * desc.d)
+        _hold_adapters(desc, w, a, b, scale, ids, count, max_rows)
+    except ValueError:
+        _check(nsc_adapter_check(desc), "nsc_adapter_backward")  # a bad description comes first
+        raise
+    p = _layer_args(stream, x, dy, w, a, b, scale, ids, count, dx, da, db, ws)
+    _check(lib().nsc_adapter_backward(ctypes.byref(desc), *p[:8], max_rows, *p[8:-1], _nbytes(ws),
+                                      p[-1]), "nsc_adapter_backward")
