@@ -378,6 +378,24 @@ typedef struct nsc_group nsc_group; /* opaque: per-camera device tables */
  * 0's, or not matching the CNN grid), NSC_E_NOMEM, NSC_E_HIP. */
 int nsc_group_create(const nsc_cascade_cfg* cfgs, const nsc_cnn* const* cnns, int32_t n_cams,
                      nsc_group** out);
+/* The cameras of a group that share one fp32 network (NSC_F32) and differ by
+ * low-rank adapters of its dense layer (its hidden units before the ReLU are
+ * nsc_adapter_project of the flattened last map, in (y, x, c) order):
+ * hidden = ReLU(x w1^T + b1 + scale[p] (x a[p]^T) b[p]^T), p the camera's
+ * adapter.  All buffers are device memory laid out as nsc_adapter_project takes
+ * them and must outlive the group; their values may change between runs. */
+typedef struct nsc_group_adapters {
+  int32_t rank, n_adapters;   /* as in nsc_adapter_desc                          */
+  const float* a;             /* [n_adapters][rank][features]                    */
+  const float* b;             /* [n_adapters][dense][rank]                       */
+  const float* scale;         /* [n_adapters]                                    */
+  const int32_t* of_camera;   /* [n_cams]: the camera's adapter, out of range
+                                 (such as -1): the shared network alone          */
+} nsc_group_adapters;
+/* As nsc_group_create with the network cnn for every camera, and adapters.
+ * Errors also NSC_E_DTYPE (a network that is not NSC_F32). */
+int nsc_group_create_shared(const nsc_cascade_cfg* cfgs, const nsc_cnn* cnn,
+                            const nsc_group_adapters* adapters, int32_t n_cams, nsc_group** out);
 /* Frees the group's tables (NULL is a no-op); no enqueued work may use it. */
 int nsc_group_destroy(nsc_group* group);
 /* State carried between consecutive nsc_group_run calls: camera c's slot

@@ -63,6 +63,11 @@ class NormDesc(ctypes.Structure):
                 ("dtype", _i32), ("eps", ctypes.c_float), ("x_stride", _i64), ("y_stride", _i64)]
 
 
+class GroupAdapters(ctypes.Structure):
+    _fields_ = [("rank", _i32), ("n_adapters", _i32), ("a", _vp), ("b", _vp), ("scale", _vp),
+                ("of_camera", _vp)]
+
+
 class AdapterDesc(ctypes.Structure):
     _fields_ = [("k", _i32), ("d", _i32), ("rank", _i32), ("n_adapters", _i32), ("dtype", _i32),
                 ("x_stride", _i64), ("y_stride", _i64)]
@@ -116,6 +121,7 @@ def lib() -> ctypes.CDLL:
             "nsc_cascade_finish": (ctypes.c_int, [_vp, _vp, _i64, _i64, _i64, _i64, _vp, _vp, _sz,
                                                   _vp, _vp, _vp, _vp, _vp, _vp]),
             "nsc_group_create": (ctypes.c_int, [_vp, _vp, _i32, _vp]),
+            "nsc_group_create_shared": (ctypes.c_int, [_vp, _vp, _vp, _i32, _vp]),
             "nsc_group_destroy": (ctypes.c_int, [_vp]),
             "nsc_group_state_bytes": (ctypes.c_int, [_vp, _vp, _vp]),
             "nsc_group_workspace_bytes": (ctypes.c_int, [_vp, _i64, _vp]),
@@ -400,6 +406,37 @@ class Group:
             self.close()
         except Exception:
             pass
+
+
+class SharedGroup(Group):
+    """A group whose cameras share one fp32 network and differ by adapters of its
+    dense layer: a [n_adapters][rank][features], b [n_adapters][dense][rank],
+    scale [n_adapters] (device, fp32) and of_camera (device, int32 per camera).
+    They must outlive the group, which keeps them."""
+
+    def __init__(self, cfgs, cnn, rank, a, b, scale, of_camera):
+        import torch
+        n_cams, n = len(cfgs), scale.numel()
+        desc = cnn.desc
+        side_h, side_w = desc.in_h, desc.in_w
+        for layer in range(desc.n_conv):
+            if desc.pool_after_mask >> layer & 1:
+                side_h, side_w = side_h // 2, side_w // 2
+        flat = desc.conv_out[desc.n_conv - 1] * side_h * side_w
+        _hold("a", a, torch.float32, n * rank * flat)
+        _hold("b", b, torch.float32, n * rank * desc.dense)
+        _hold("scale", scale, torch.float32, n)
+        _hold("of_camera", of_camera, torch.int32, n_cams)
+        self.n_cams = n_cams
+        self._cfgs = (CascadeCfg * n_cams)(*cfgs)
+        self.cnns = [cnn]
+        self.adapters = (a, b, scale, of_camera)
+        ad = GroupAdapters(rank, n, _ptr(a), _ptr(b), _ptr(scale), _ptr(of_camera))
+        h = _vp()
+        self.handle = None
+        _check(lib().nsc_group_create_shared(self._cfgs, cnn.handle, ctypes.byref(ad), n_cams,
+                                             ctypes.byref(h)), "nsc_group_create_shared")
+        self.handle = h
 
 
 def nsc_group_create_status(cfgs, cnn_handles) -> int:

@@ -1168,6 +1168,8 @@ struct nsc_group {
   void* dev;             // CamDiff[n_cams], then CamNet[n_cams]
   CamDiff* cams;
   CamNet* nets;
+  bool shared;           // one network with adapters
+  nsc_group_adapters ad;
 };
 
 namespace nsc {
@@ -1175,7 +1177,9 @@ namespace {
 
 // Workspace of a group run of n frames per camera.
 struct GroupLayout {
-  size_t sums, fire, dec, idx, count, tiles, logit, scratch, cnn, total;
+  size_t sums, fire, dec, idx, count, tiles, logit, scratch, cnn, cnn_end;
+  size_t ids, hidden, adapt, adapt_bytes;  // shared network with adapters
+  size_t total;
 };
 
 GroupLayout group_layout(const nsc_group* g, int64_t n) {
@@ -1197,6 +1201,14 @@ GroupLayout group_layout(const nsc_group* g, int64_t n) {
   L.logit = take((size_t)N * 4);
   L.scratch = take(g->max_delta > 0 ? (size_t)g->n_cams * (size_t)g->slot : 0);
   L.cnn = take(cnn_workspace_bytes(g->base->c, N));
+  L.cnn_end = o;
+  if (g->shared) {
+    const nsc_adapter_desc d = shared_desc(g->base->c, g->ad);
+    nsc_adapter_workspace_bytes(&d, N, 0, &L.adapt_bytes);  // checked when the group was made
+    L.ids = take((size_t)N * 4);
+    L.hidden = take((size_t)N * g->base->c.dense * 4);
+    L.adapt = take(L.adapt_bytes);
+  }
   L.total = o;
   return L;
 }
@@ -1310,6 +1322,33 @@ int nsc_group_create(const nsc_cascade_cfg* cfgs, const nsc_cnn* const* cnns, in
   g->dev = dev;
   g->cams = reinterpret_cast<CamDiff*>(b);
   g->nets = reinterpret_cast<CamNet*>(b + diff_bytes);
+  *out = g;
+  return NSC_OK;
+}
+
+int nsc_group_create_shared(const nsc_cascade_cfg* cfgs, const nsc_cnn* cnn,
+                            const nsc_group_adapters* ad, int32_t n_cams, nsc_group** out) {
+  g_err[0] = 0;
+  NSC_REQUIRE(out != nullptr && cfgs != nullptr && ad != nullptr, NSC_E_INVAL,
+              "cfgs, adapters or out is NULL");
+  *out = nullptr;
+  NSC_REQUIRE(n_cams >= 1 && n_cams <= NSC_MAX_CAMERAS, NSC_E_INVAL, "n_cams %d outside 1..%d",
+              n_cams, NSC_MAX_CAMERAS);
+  NSC_REQUIRE(ad->a && ad->b && ad->scale && ad->of_camera, NSC_E_INVAL,
+              "an adapter buffer is NULL");
+  NSC_REQUIRE(((uintptr_t)ad->a | (uintptr_t)ad->b | (uintptr_t)ad->scale |
+               (uintptr_t)ad->of_camera) % 4 == 0, NSC_E_INVAL,
+              "an adapter buffer is not aligned to its elements");
+  NSC_REQUIRE(cnn != nullptr, NSC_E_INVAL, "network handle is NULL");
+  NSC_REQUIRE(cnn->c.desc.dtype == NSC_F32, NSC_E_DTYPE,
+              "a shared network with adapters is NSC_F32, not dtype %d", cnn->c.desc.dtype);
+  const nsc_adapter_desc d = shared_desc(cnn->c, *ad);
+  if (int rc = nsc_adapter_check(&d)) return rc;
+  std::vector<const nsc_cnn*> cnns((size_t)n_cams, cnn);
+  nsc_group* g = nullptr;
+  if (int rc = nsc_group_create(cfgs, cnns.data(), n_cams, &g)) return rc;
+  g->shared = true;
+  g->ad = *ad;
   *out = g;
   return NSC_OK;
 }
@@ -1432,7 +1471,16 @@ int nsc_group_run(const nsc_group* g, const uint8_t* frames, int64_t n, int64_t 
   r.nets = g->nets;
   r.per_cam = n;
   r.n_nets = g->n_cams;
-  if (int rc = run_cnn(c, r, w + L.cnn, L.total - L.cnn, st)) return rc;
+  SharedDense sd{};
+  if (g->shared) {
+    sd.ad = g->ad;
+    sd.ids = reinterpret_cast<int32_t*>(w + L.ids);
+    sd.hidden = reinterpret_cast<float*>(w + L.hidden);
+    sd.ws = w + L.adapt;
+    sd.ws_bytes = L.adapt_bytes;
+    r.shared = &sd;
+  }
+  if (int rc = run_cnn(c, r, w + L.cnn, L.cnn_end - L.cnn, st)) return rc;
   if (int rc = mark(4)) return rc;
   // 5: decisions of the frames that did not fire, then the cameras' state
   if (int rc = launch_group_resolve(g->cams, g->n_cams, g->max_delta, fire, dec, sums, cells, n, t0,

@@ -2864,6 +2864,39 @@ __global__ void __launch_bounds__(64 * kDenseFinWaves) k_dense_finish(DenseArgs 
   }
 }
 
+// A shared network with adapters: the adapter of each survivor's camera.
+__global__ void __launch_bounds__(256) k_slot_adapters(DenseArgs a, const int32_t* of_camera,
+                                                       int32_t* ids) {
+  int64_t cnt = *a.count;
+  if (cnt > a.max_count) cnt = a.max_count;
+  for (int64_t s = blockIdx.x * 256ll + threadIdx.x; s < cnt; s += gridDim.x * 256ll)
+    ids[s] = of_camera[cam_at(a, s)];
+}
+// Its output layer on the hidden units' pre-activations: a wave per survivor,
+// with the thresholds of its camera.
+__global__ void __launch_bounds__(256) k_shared_head(DenseArgs a, const float* hidden,
+                                                     int32_t dense) {
+  int64_t cnt = *a.count;
+  if (cnt > a.max_count) cnt = a.max_count;
+  const int lane = threadIdx.x & 63;
+  for (int64_t s = blockIdx.x * 4ll + (threadIdx.x >> 6); s < cnt; s += gridDim.x * 4ll) {
+    float sum = 0.0f;
+    for (int u = lane; u < dense; u += 64)
+      sum += a.w2[u] * fmaxf(hidden[s * dense + u], 0.0f);
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o, 64);
+    if (lane == 0) {
+      const CamNet& cn = a.nets[cam_at(a, s)];
+      const float z = sum + a.b2;
+      const double p = 1.0 / (1.0 + exp(-(double)z));
+      const int32_t f = a.idx[s];
+      a.logit[s] = z;
+      if (a.dec) a.dec[f] = p < cn.c_low ? 0 : (p > cn.c_high ? 1 : 2);
+      if (a.frame_logit) a.frame_logit[f] = z;
+    }
+  }
+}
+
 template <typename T, bool FIRST>
 int launch_conv_nt(int nt, const ConvArgs& a, unsigned grid, size_t lds, hipStream_t st) {
 #define NSC_CONV_CASE(N)                                                                       \
@@ -3440,6 +3473,11 @@ size_t cnn_dense_part_bytes(const Cnn& cnn, int64_t max_count) {
   return n;
 }
 
+nsc_adapter_desc shared_desc(const Cnn& cnn, const nsc_group_adapters& ad) {
+  return nsc_adapter_desc{cnn.flat, cnn.dense, ad.rank, ad.n_adapters, NSC_T_F32, cnn.flat,
+                          cnn.dense};
+}
+
 size_t cnn_workspace_bytes(const Cnn& cnn, int64_t max_count) {
   const size_t per = align_up(cnn.act_elems * sizeof(float), 256);
   return 2 * per * (size_t)(max_count > 0 ? max_count : 0) + 256 + cnn_xin_bytes(cnn, max_count) +
@@ -3479,7 +3517,7 @@ int run_cnn(const Cnn& cnn, const CnnRunArgs& r, void* ws, size_t ws_bytes, hipS
     a.pool = L.pool ? 1 : 0;
     conv_tiles(L, &a.tiles_y, &a.tiles_x);
     a.scl = cnn.scales + 2 * l;
-    a.nets = r.nets;
+    a.nets = r.shared ? nullptr : r.nets;  // the shared network is the base one
     a.per_cam = r.per_cam;
     a.overflow = cnn.overflow;
     return a;
@@ -3662,6 +3700,25 @@ int run_cnn(const Cnn& cnn, const CnnRunArgs& r, void* ws, size_t ws_bytes, hipS
   d.c_high = r.c_high;
   d.nets = r.nets;
   d.per_cam = r.per_cam;
+  if (r.shared) {
+    const SharedDense& sd = *r.shared;
+    int64_t grid = (r.max_count + 255) / 256;
+    if (grid > kNumCU * 8) grid = kNumCU * 8;
+    hipLaunchKernelGGL(k_slot_adapters, dim3((unsigned)grid), dim3(256), 0, stream, d,
+                       sd.ad.of_camera, sd.ids);
+    NSC_CHECK_LAUNCH("k_slot_adapters");
+    const nsc_adapter_desc desc = shared_desc(cnn, sd.ad);
+    if (int rc = nsc_adapter_project(&desc, d.feat, cnn.w1, cnn.b1, sd.ad.a, sd.ad.b, sd.ad.scale,
+                                     sd.ids, r.count, r.max_count, sd.hidden, sd.ws, sd.ws_bytes,
+                                     stream))
+      return rc;
+    grid = (r.max_count + 3) / 4;
+    if (grid > kNumCU * 16) grid = kNumCU * 16;
+    hipLaunchKernelGGL(k_shared_head, dim3((unsigned)grid), dim3(256), 0, stream, d, sd.hidden,
+                       cnn.dense);
+    NSC_CHECK_LAUNCH("k_shared_head");
+    return NSC_OK;
+  }
   const int nt = cnn.dense / 16;
   f32x4* part = reinterpret_cast<f32x4*>(static_cast<unsigned char*>(ws) +
                                          2 * per * (size_t)r.max_count + 256 +

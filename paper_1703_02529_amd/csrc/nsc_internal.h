@@ -295,6 +295,18 @@ struct CamNet {
   int32_t overflow;         // Cnn::overflow of the camera's network
 };
 
+// A camera group's shared network with adapters of its dense layer: the
+// adapters and, in the workspace, the survivors' adapters, their hidden units
+// and the operator's own workspace.
+struct SharedDense {
+  nsc_group_adapters ad;
+  int32_t* ids;
+  float* hidden;
+  void* ws;
+  size_t ws_bytes;
+};
+nsc_adapter_desc shared_desc(const Cnn& cnn, const nsc_group_adapters& ad);
+
 struct CnnRunArgs {
   const int32_t* sums;
   int32_t sums_h, sums_w, fy, fx;
@@ -313,6 +325,7 @@ struct CnnRunArgs {
   const CamNet* nets;
   int64_t per_cam;
   int32_t n_nets;           // cameras of the group (0 without a group)
+  const SharedDense* shared;  // the cameras share the base network (else null)
 };
 size_t cnn_workspace_bytes(const Cnn& cnn, int64_t max_count);
 int run_cnn(const Cnn& cnn, const CnnRunArgs& a, void* ws, size_t ws_bytes, hipStream_t stream);

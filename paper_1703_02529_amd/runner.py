@@ -12,7 +12,8 @@ from typing import Optional
 
 import torch
 
-from . import (NSC_METRIC_MSE, NSC_REF_FIXED, NSC_REF_PREV, Cnn, Group, make_cfg, make_desc,
+from . import (NSC_METRIC_MSE, NSC_REF_FIXED, NSC_REF_PREV, Cnn, Group, SharedGroup, make_cfg,
+               make_desc,
                nsc_batch_workspace_bytes, nsc_cascade_finish, nsc_cascade_run,
                nsc_cascade_stage, nsc_cascade_workspace_bytes, nsc_group_run,
                nsc_group_state_bytes, nsc_group_workspace_bytes, nsc_state_bytes)
@@ -107,10 +108,12 @@ class GroupRunner:
     """Buffers of a camera group: one workload description per camera (same
     frame geometry and metric), each with its weight blob and its device LR
     weights / reference sums (None where unused).  Runs n frames of every
-    camera per call, camera-major."""
+    camera per call, camera-major.  With adapters = (rank, a, b, scale,
+    of_camera), as SharedGroup takes them, the cameras share the one network of
+    blobs[0]."""
 
     def __init__(self, wls, blobs, frames_per_cam: int, lr_ws=None, ref_sums=None,
-                 device="cuda"):
+                 device="cuda", adapters=None):
         self.wls = list(wls)
         k = len(self.wls)
         self.device = torch.device(device)
@@ -119,7 +122,10 @@ class GroupRunner:
         self.cfgs = [_cfg_of(w, l, r) for w, l, r in zip(self.wls, self.lr_ws, self.ref_sums)]
         self.cnns = [Cnn(make_desc(w.cnn.conv, w.cnn.pool, w.cnn.dense, w.cnn.in_h, w.cnn.in_w,
                                    w.cnn.bf16), b) for w, b in zip(self.wls, blobs)]
-        self.group = Group(self.cfgs, self.cnns)
+        if adapters is None:
+            self.group = Group(self.cfgs, self.cnns)
+        else:
+            self.group = SharedGroup(self.cfgs, self.cnns[0], *adapters)
         self.frames_per_cam = frames_per_cam
         total = k * frames_per_cam
         ws = nsc_group_workspace_bytes(self.group, frames_per_cam)
