@@ -384,7 +384,7 @@ __global__ void __launch_bounds__(1024) k_norm(NormArgs a) {
 // ---------------------------------------------------------------- backward
 
 template <typename T, int VE, int K, bool RAG, int V, NormPass P>
-__global__ void __launch_bounds__(512) k_norm_grad(NormArgs a) {
+__global__ void __launch_bounds__(VE == 1 ? 1024 : 512) k_norm_grad(NormArgs a) {
   extern __shared__ __align__(16) float sm[];  // [2 VE][blockDim], then [cb][2], then [gpb][2]
   const int T_ = blockDim.x;
   float* chs = sm + (P == NormPass::Apply ? 0 : 2 * VE * T_);
@@ -704,7 +704,7 @@ NormPlan plan_norm(const nsc_norm_desc& d, uintptr_t ptrs, int64_t max_count, bo
   p.parts = 1;
   const int64_t items = max_count * p.blocks, bytes = hw * p.cb * es;
   if (p.threads == 1024 && items < 2 * kNumCU && bytes > 32768) p.v = 0;
-  if (p.v == 0) p.threads = p.cv > 512 ? most_t : 512;
+  if (p.v == 0) p.threads = p.cv > 512 ? 1024 : 512;  // over 512: single elements
   if (items > 0 && p.v == 0 && items < 2 * kNumCU) {
     int64_t parts = (4 * kNumCU + items - 1) / items;
     if (parts > bytes / 16384) parts = bytes / 16384;
@@ -713,7 +713,7 @@ NormPlan plan_norm(const nsc_norm_desc& d, uintptr_t ptrs, int64_t max_count, bo
     if (parts > 1) {
       p.parts = (int32_t)parts;
       const int32_t t = items * parts >= 3 * kNumCU ? 256 : items * parts > kNumCU ? 512 : most_t;
-      if (p.cv <= t) p.threads = t;
+      if (p.cv <= t && p.threads < 1024) p.threads = t;
     }
   }
   p.pl = p.threads / p.cv;

@@ -159,6 +159,20 @@ def test_strides_alignment_and_counts(dtype, pad, shift, live):
     untouched(m, m.dx)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("form", [(2, 3, 3, 1024, 1), (1, 40, 40, 700, 1), (3, 2, 2, 1023, 1)],
+                         ids=str)
+def test_wide_groups_off_every_alignment(form, dtype):
+    """Groups of more channels than half a workgroup, one element at a time."""
+    m = Maps(*form, dtype=dtype, act="relu", pad=1, shift=1)
+    m.forward()
+    check_forward(m)
+    untouched(m, m.y)
+    m.backward()
+    check_backward(m)
+    untouched(m, m.dx)
+
+
 def test_in_place_and_without_statistics():
     m = Maps(6, 30, 30, 64, 8)
     m.forward()
