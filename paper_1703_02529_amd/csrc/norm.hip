@@ -668,7 +668,8 @@ NormPlan plan_norm(const nsc_norm_desc& d, uintptr_t ptrs, int64_t max_count, bo
     if (hw * p.gpb * cpg * es > (int64_t)most_t * most_v * 16) {
       // too large for registers: with few images as contiguous as can be (they
       // are split by pixels), else as above
-      if (max_count * (d.groups / p.gpb) < 2 * kNumCU) p.gpb = groups_for(4096);
+      const int32_t g = groups_for(4096);
+      if (g > 0 && max_count * (d.groups / p.gpb) < 2 * kNumCU) p.gpb = g;
     } else {
       for (int64_t bytes = 64; bytes >= 16; bytes /= 2) {
         if (max_count * (d.groups / p.gpb) >= kNumCU || hw * p.gpb * cpg * es <= 8192) break;

@@ -87,6 +87,21 @@ def test_norm_workspace_sizes():
                                                     ctypes.byref(b)) == nsc.NSC_E_INVAL
 
 
+@pytest.mark.parametrize("dtype", [nsc.NSC_T_F32, nsc.NSC_T_BF16])
+@pytest.mark.parametrize("side", [(1, 1), (3, 5), (40, 40), (300, 200)])
+def test_norm_workspaces_of_every_form(side, dtype):
+    """A workspace is found for all channel counts, groups and strides."""
+    for c, groups in ((1, 1), (17, 1), (45, 5), (64, 8), (513, 1), (700, 1), (1021, 1021),
+                      (1024, 1), (2046, 2), (2040, 2040), (4096, 64), (65536, 64)):
+        for pad in (0, 1, 2, 8):
+            d = _norm(h=side[0], w=side[1], c=c, groups=groups, dtype=dtype,
+                      x_stride=side[0] * side[1] * c + pad)
+            for n in (1, 3, 300, 5000):
+                for backward in (False, True):
+                    got = nsc.nsc_group_norm_workspace_bytes(d, n, backward=backward)
+                    assert got >= (8 * n * c if backward else 0)
+
+
 def _adapter(**kw):
     base = dict(k=4608, d=128, rank=8, n_adapters=24, dtype=nsc.NSC_T_BF16)
     base.update(kw)
