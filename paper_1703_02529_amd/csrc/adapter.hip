@@ -1018,14 +1018,15 @@ GemmPlan plan_gemm(int64_t max_rows, int64_t outs, int64_t len, int64_t es, bool
     return (outs + tn - 1) / tn * ((max_rows + tm - 1) / tm);
   };
   const int64_t blocks = (len * es + 127) / 128;
-  const bool big = tiles(256, 128) >= kNumCU && blocks >= 16;
+  const bool few = !tr && outs <= 64 && max_rows > 16;
+  const bool big = !few && tiles(256, 128) >= kNumCU && blocks >= 16;
   p.tn = big ? 256 : 128;
   p.tm = big ? 128 : max_rows <= 16 ? 16 : 64;
   // Up to 64 outputs would leave half of a tile of 128 to multiply zeros, which
   // counts where the matrix instructions are slow: 3,038 rows of 4,608 values
   // onto 32 outputs in fp32 took 91 us with 128 and take 61 with 64.  Backward
   // the tiles run over the inputs, which are many.
-  if (!tr && outs <= 64 && p.tm == 64) p.tn = 64;
+  if (few) p.tn = 64;
   const int64_t t = tiles(p.tn, p.tm);
   // parts for about a workgroup per CU, each of at least four blocks
   int64_t parts = t > 0 ? kNumCU / t : 1;

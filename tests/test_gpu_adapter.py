@@ -166,7 +166,8 @@ def test_forward_and_backward(form, order, dtype):
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("form", [(2050, 1152, 1088, 16, 6), (1100, 776, 520, 24, 70),
-                                  (1030, 136, 8264, 16, 6), (1030, 8260, 140, 24, 5)], ids=str)
+                                  (1030, 136, 8264, 16, 6), (1030, 8260, 140, 24, 5),
+                                  (32900, 1032, 40, 8, 5)], ids=str)
 def test_many_rows(form, dtype):
     r = Rows(*form, dtype=dtype, order="mixed")
     r.forward()
