@@ -22,6 +22,7 @@
 // hold them.  A few large images are split over workgroups that leave their
 // parts' statistics in the workspace for a second launch to join.
 #include "layer_types.h"
+#include "norm_plan.h"
 
 #include <math.h>
 
@@ -110,7 +111,7 @@ struct Place {
   }
   // Values of the thread's vector that lie inside the image at step p.
   __device__ __forceinline__ int inside(const NormArgs& a, int p) const {
-    return RAG ? min(VE, a.hw * a.c - (p * a.s * a.c + v * VE)) : VE;
+    return RAG ? values_inside(a.hw, a.c, a.s, a.steps, p, v * VE, VE) : VE;
   }
   __device__ __forceinline__ int64_t offset(const NormArgs& a, int p) const {
     return (int64_t)p * a.s * a.c + ch0 + v * VE;
