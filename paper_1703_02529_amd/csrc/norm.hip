@@ -748,8 +748,10 @@ NormArgs norm_args(const nsc_norm_desc& d, const NormPlan& p, const int32_t* cou
 
 template <typename T, int VE, int K, bool RAG, int V, NormPass P>
 int launch_norm(const NormArgs& a, const NormPlan& p, bool backward, hipStream_t st) {
+  // (a launch has fewer than 2^32 threads; its workgroups take the items behind)
   int64_t grid = a.max_count * p.blocks * p.parts;
-  if (grid > 0x7FFFFFFF) grid = 0x7FFFFFFF;
+  const int64_t most = 0xFFFFFFFFll / p.threads;
+  if (grid > most) grid = most;
   const dim3 g((unsigned)grid), b((unsigned)p.threads);
   if (backward) {
     if constexpr (V <= 10) {
