@@ -111,6 +111,7 @@ struct AdapterArgs {
   int64_t row_tiles;        // the product's grid: out_tiles x row_tiles x parts, after
   int32_t out_tiles;        // down_blocks workgroups of rank-wide rows
   int32_t down_blocks, down_sets;
+  int64_t first;            // the launch's first workgroup of them
 };
 
 __device__ __forceinline__ int64_t live_rows(const AdapterArgs& a) {
@@ -612,7 +613,7 @@ __global__ void __launch_bounds__(TN >= 256 ? 512 : 256) k_adapter_gemm(AdapterA
   __shared__ uint4 stage0[kStage], stage1[kStage], stage2[ST > 2 ? kStage : 1];
   __shared__ uint4 stage3[ST > 3 ? kStage : 1];
   uint4* const last = ST > 3 ? stage3 : ST > 2 ? stage2 : stage1;
-  int64_t block = blockIdx.x;
+  int64_t block = a.first + blockIdx.x;
   if constexpr (!TR && TN < 256) {  // a call whose product is split takes its rank-wide rows here
     if (block < a.down_blocks) {
       static_assert(kStage >= kGemmDownWaves * 256 && kGemmDownWaves * 64 == TH, "in the stages");
@@ -814,21 +815,25 @@ __global__ void __launch_bounds__(256) k_adapter_join(AdapterArgs a) {
 constexpr int kListWaves = 16;
 
 // b[p] [d][rank] as [rank][d], 64 rows at a time through LDS: the rank-wide
-// rows u then read b as t read a.
+// rows u then read b as t read a.  Of all such items, every `of`-th from `item`.
 template <typename T>
-__device__ __forceinline__ void adapter_flip(const AdapterArgs& a, int64_t item, T* bt) {
+__device__ __forceinline__ void adapter_flip(const AdapterArgs& a, int64_t item, int64_t of,
+                                             T* bt) {
   __shared__ T tile[64 * (NSC_MAX_RANK + 1)];
   const int blocks = (a.d + 63) / 64;
-  const int64_t p = item / blocks;
-  const int d0 = (int)(item % blocks) * 64, nd = min(64, a.d - d0);
-  const T* from = static_cast<const T*>(a.b) + (p * a.d + d0) * a.rank;
-  for (int i = threadIdx.x; i < nd * a.rank; i += 64 * kListWaves)
-    tile[i / a.rank * (a.rank + 1) + i % a.rank] = from[i];
-  __syncthreads();
-  T* to = bt + p * a.rank * a.d + d0;
-  for (int i = threadIdx.x; i < 64 * a.rank; i += 64 * kListWaves) {
-    const int j = i / 64, r = i % 64;
-    if (r < nd) to[(int64_t)j * a.d + r] = tile[r * (a.rank + 1) + j];
+  for (; item < (int64_t)a.n_adapters * blocks; item += of) {
+    const int64_t p = item / blocks;
+    const int d0 = (int)(item % blocks) * 64, nd = min(64, a.d - d0);
+    const T* from = static_cast<const T*>(a.b) + (p * a.d + d0) * a.rank;
+    for (int i = threadIdx.x; i < nd * a.rank; i += 64 * kListWaves)
+      tile[i / a.rank * (a.rank + 1) + i % a.rank] = from[i];
+    __syncthreads();
+    T* to = bt + p * a.rank * a.d + d0;
+    for (int i = threadIdx.x; i < 64 * a.rank; i += 64 * kListWaves) {
+      const int j = i / 64, r = i % 64;
+      if (r < nd) to[(int64_t)j * a.d + r] = tile[r * (a.rank + 1) + j];
+    }
+    __syncthreads();  // the tile is read before the next item writes it
   }
 }
 
@@ -836,7 +841,8 @@ template <typename T>
 __global__ void __launch_bounds__(64 * kListWaves) k_adapter_list(AdapterArgs a, int32_t* off,
                                                                   int32_t* rows, int32_t listers,
                                                                   T* bt) {
-  if ((int)blockIdx.x >= listers) return adapter_flip<T>(a, blockIdx.x - listers, bt);
+  if ((int)blockIdx.x >= listers)
+    return adapter_flip<T>(a, blockIdx.x - listers, gridDim.x - listers, bt);
   __shared__ int32_t less[kListWaves], same[kListWaves];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int64_t n = live_rows(a);
@@ -983,6 +989,7 @@ __global__ void __launch_bounds__(512) k_adapter_grad(GradArgs a) {
 // -------------------------------------------------------------------- host
 
 constexpr int64_t kMaxRows = 0x7FFFFFFF;
+constexpr int64_t kLaunchThreads = 0xFFFFFFFFll;  // of one launch
 
 bool misaligned(const void* p, int64_t bytes) { return (uintptr_t)p % (uintptr_t)bytes != 0; }
 
@@ -1126,12 +1133,13 @@ int launch_tiles(AdapterArgs a, hipStream_t st) {
   a.out_tiles = ((TR ? a.k : a.d) + TN - 1) / TN;
   a.row_tiles = (a.max_rows + TM - 1) / TM;
   const int64_t tiles = a.out_tiles * a.row_tiles, grid = tiles * a.parts + a.down_blocks;
-  if (grid > 0x7FFFFFFF)
-    return fail(NSC_E_SHAPE, "%lld rows onto %d outputs are more tiles than a launch holds",
-                (long long)a.max_rows, TR ? a.k : a.d);
-  hipLaunchKernelGGL((k_adapter_gemm<T, VEC, TR, TN, TM>), dim3((unsigned)grid),
-                     dim3(G::kThreads), 0, st, a);
-  NSC_CHECK_LAUNCH("k_adapter_gemm");
+  const int64_t most = kLaunchThreads / G::kThreads;  // in launches of that many
+  for (a.first = 0; a.first < grid; a.first += most) {
+    hipLaunchKernelGGL((k_adapter_gemm<T, VEC, TR, TN, TM>),
+                       dim3((unsigned)(grid - a.first < most ? grid - a.first : most)),
+                       dim3(G::kThreads), 0, st, a);
+    NSC_CHECK_LAUNCH("k_adapter_gemm");
+  }
   if constexpr (TN < 256) {
     if (a.parts > 1) {
       hipLaunchKernelGGL((k_adapter_join<T, TR, TN, TM>),
@@ -1182,10 +1190,9 @@ int launch_grad(GradArgs a, int32_t n_adapters, int64_t max_rows, hipStream_t st
 template <typename T>
 int launch_list(AdapterArgs* a, int32_t* off, int32_t* rows, T* bt, hipStream_t st) {
   const int32_t most = 8 * kNumCU, listers = a->n_adapters < most ? a->n_adapters + 1 : most;
-  const int64_t flips = bt ? (int64_t)a->n_adapters * ((a->d + 63) / 64) : 0;
-  if (listers + flips > 0x7FFFFFFF)
-    return fail(NSC_E_SHAPE, "%d adapters of %d outputs are more than a launch holds",
-                a->n_adapters, a->d);
+  int64_t flips = bt ? (int64_t)a->n_adapters * ((a->d + 63) / 64) : 0;
+  const int64_t room = kLaunchThreads / (64 * kListWaves) - listers;
+  if (flips > room) flips = room;  // its workgroups take the ones behind
   hipLaunchKernelGGL(k_adapter_list<T>, dim3((unsigned)(listers + flips)), dim3(64 * kListWaves), 0,
                      st, *a, off, rows, listers, bt);
   NSC_CHECK_LAUNCH("k_adapter_list");
