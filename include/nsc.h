@@ -537,7 +537,7 @@ typedef struct nsc_adapter_desc {
 /* Validates a description without touching the GPU. */
 int nsc_adapter_check(const nsc_adapter_desc* desc);
 /* Workspace of nsc_adapter_project (backward = 0) or nsc_adapter_backward
- * (backward = 1) for up to max_rows rows. */
+ * (backward = 1) for up to max_rows rows: at most 2^31 - 1, backward 2^31 - 256. */
 int nsc_adapter_workspace_bytes(const nsc_adapter_desc* desc, int64_t max_rows, int32_t backward,
                                 size_t* bytes);
 /* With p = ids[r] the adapter of row r,

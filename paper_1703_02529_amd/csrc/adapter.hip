@@ -989,6 +989,9 @@ __global__ void __launch_bounds__(512) k_adapter_grad(GradArgs a) {
 // -------------------------------------------------------------------- host
 
 constexpr int64_t kMaxRows = 0x7FFFFFFF;
+// Backward: k_adapter_grad looks up to 16 x 8 + 15 positions past the last row,
+// in 32 bits.
+constexpr int64_t kMaxGradRows = kMaxRows - 255;
 constexpr int64_t kLaunchThreads = 0xFFFFFFFFll;  // of one launch
 
 bool misaligned(const void* p, int64_t bytes) { return (uintptr_t)p % (uintptr_t)bytes != 0; }
@@ -1106,8 +1109,8 @@ AdapterLayout adapter_layout(const nsc_adapter_desc& d, int64_t max_rows, bool b
 int check_adapter_call(const nsc_adapter_desc* d, int64_t max_rows, const void* ws,
                        size_t ws_bytes, bool backward) {
   if (int rc = check_adapter(d)) return rc;
-  NSC_REQUIRE_L(max_rows >= 0 && max_rows <= kMaxRows, NSC_E_INVAL, "max_rows %lld out of range",
-                (long long)max_rows);
+  NSC_REQUIRE_L(max_rows >= 0 && max_rows <= (backward ? kMaxGradRows : kMaxRows), NSC_E_INVAL,
+                "max_rows %lld out of range", (long long)max_rows);
   const size_t need = adapter_layout(*d, max_rows, backward).total;
   NSC_REQUIRE_L(need == 0 || (ws != nullptr && (uintptr_t)ws % 256 == 0 && ws_bytes >= need),
                 NSC_E_WORKSPACE, "workspace needs %zu bytes (256-byte aligned), got %zu", need,
@@ -1327,8 +1330,8 @@ int nsc_adapter_workspace_bytes(const nsc_adapter_desc* desc, int64_t max_rows, 
                                 size_t* bytes) {
   fail(NSC_OK, "%s", "");
   if (int rc = check_adapter(desc)) return rc;
-  NSC_REQUIRE_L(bytes != nullptr && max_rows >= 0 && max_rows <= kMaxRows &&
-                    (backward == 0 || backward == 1),
+  NSC_REQUIRE_L(bytes != nullptr && max_rows >= 0 && (backward == 0 || backward == 1) &&
+                    max_rows <= (backward ? kMaxGradRows : kMaxRows),
                 NSC_E_INVAL, "bad arguments");
   *bytes = adapter_layout(*desc, max_rows, backward != 0).total;
   return NSC_OK;

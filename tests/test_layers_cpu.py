@@ -175,3 +175,16 @@ def test_the_binding_refuses_host_tensors_and_short_buffers():
         nsc.nsc_group_norm(n, m, m, m, m, None, 2)
     with pytest.raises(ValueError, match="gamma:"):
         nsc.nsc_group_norm(n, m, m, m, m, None, 1)
+
+
+def test_the_gradients_take_fewer_rows_than_32_bits_count():
+    """Positions are looked up past the last row, in 32 bits: 2^31 - 256 rows are
+    the most that nsc_adapter_backward takes."""
+    d = _adapter(k=1, d=1, rank=1, n_adapters=1)
+    most = 2 ** 31 - 256
+    assert nsc.nsc_adapter_workspace_bytes(d, most, backward=True) > 2 * 64 * most
+    assert nsc.nsc_adapter_workspace_bytes(d, 2 ** 31 - 1) > 64 * most
+    for n in (most + 1, 2 ** 31 - 1):
+        assert _project_bwd(d, n=n, ws_bytes=1 << 60) == nsc.NSC_E_INVAL
+        with pytest.raises(nsc.NscError):
+            nsc.nsc_adapter_workspace_bytes(d, n, backward=True)
