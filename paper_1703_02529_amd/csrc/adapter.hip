@@ -1106,6 +1106,19 @@ AdapterLayout adapter_layout(const nsc_adapter_desc& d, int64_t max_rows, bool b
   return L;
 }
 
+// Of every call of up to max_rows rows.  Fewer rows are split into more parts,
+// so that a smaller call can need more.  Between multiples of 16 rows a call
+// only grows, and from 8,192 rows on neither reduction is split: 128 tiles of 64
+// rows leave a tile fewer than two parts, 512 tiles of 16 its rank-wide rows.
+size_t adapter_ws_bytes(const nsc_adapter_desc& d, int64_t max_rows, bool backward) {
+  size_t most = adapter_layout(d, max_rows, backward).total;
+  for (int64_t n = 16; n < max_rows && n <= 8192; n += 16) {
+    const size_t b = adapter_layout(d, n, backward).total;
+    if (b > most) most = b;
+  }
+  return most;
+}
+
 int check_adapter_call(const nsc_adapter_desc* d, int64_t max_rows, const void* ws,
                        size_t ws_bytes, bool backward) {
   if (int rc = check_adapter(d)) return rc;
@@ -1315,6 +1328,11 @@ int backward(const nsc_adapter_desc& d, AdapterArgs a, const void* x, const void
 }
 
 }  // namespace
+
+size_t adapter_call_bytes(const nsc_adapter_desc& d, int64_t rows) {
+  return adapter_layout(d, rows, false).total;
+}
+
 }  // namespace nsc
 
 using namespace nsc;
@@ -1333,7 +1351,7 @@ int nsc_adapter_workspace_bytes(const nsc_adapter_desc* desc, int64_t max_rows, 
   NSC_REQUIRE_L(bytes != nullptr && max_rows >= 0 && (backward == 0 || backward == 1) &&
                     max_rows <= (backward ? kMaxGradRows : kMaxRows),
                 NSC_E_INVAL, "bad arguments");
-  *bytes = adapter_layout(*desc, max_rows, backward != 0).total;
+  *bytes = adapter_ws_bytes(*desc, max_rows, backward != 0);
   return NSC_OK;
 }
 

@@ -1175,14 +1175,15 @@ struct nsc_group {
 namespace nsc {
 namespace {
 
-// Workspace of a group run of n frames per camera.
+// Workspace of a group run of n frames per camera; up_to: room for the adapters
+// of every run of fewer as well.
 struct GroupLayout {
   size_t sums, fire, dec, idx, count, tiles, logit, scratch, cnn, cnn_end;
   size_t ids, hidden, adapt, adapt_bytes;  // shared network with adapters
   size_t total;
 };
 
-GroupLayout group_layout(const nsc_group* g, int64_t n) {
+GroupLayout group_layout(const nsc_group* g, int64_t n, bool up_to) {
   GroupLayout L{};
   const int64_t N = (int64_t)g->n_cams * n;
   const size_t cells = (size_t)g->geo.dd_h * g->geo.dd_w * 3;
@@ -1204,7 +1205,9 @@ GroupLayout group_layout(const nsc_group* g, int64_t n) {
   L.cnn_end = o;
   if (g->shared) {
     const nsc_adapter_desc d = shared_desc(g->base->c, g->ad);
-    nsc_adapter_workspace_bytes(&d, N, 0, &L.adapt_bytes);  // checked when the group was made
+    L.adapt_bytes = adapter_call_bytes(d, N);
+    if (up_to)  // (checked when the group was made)
+      nsc_adapter_workspace_bytes(&d, N, 0, &L.adapt_bytes);
     L.ids = take((size_t)N * 4);
     L.hidden = take((size_t)N * g->base->c.dense * 4);
     L.adapt = take(L.adapt_bytes);
@@ -1376,7 +1379,7 @@ int nsc_group_workspace_bytes(const nsc_group* g, int64_t frames_per_cam, size_t
   NSC_REQUIRE(frames_per_cam >= 0 && frames_per_cam <= kMaxFrames / g->n_cams, NSC_E_INVAL,
               "frames_per_cam %lld out of range for %d cameras", (long long)frames_per_cam,
               g->n_cams);
-  *bytes = group_layout(g, frames_per_cam).total;
+  *bytes = group_layout(g, frames_per_cam, true).total;
   return NSC_OK;
 }
 
@@ -1402,7 +1405,7 @@ int nsc_group_run(const nsc_group* g, const uint8_t* frames, int64_t n, int64_t 
               "frames, label_out or defer_out is NULL");
   NSC_REQUIRE(!(g->max_delta > 0 && state == nullptr), NSC_E_STATE,
               "a camera compares with earlier frames: the group needs a state buffer");
-  const GroupLayout L = group_layout(g, n);
+  const GroupLayout L = group_layout(g, n, false);
   NSC_REQUIRE(ws != nullptr && ((uintptr_t)ws % kAlign) == 0 && ws_bytes >= L.total,
               NSC_E_WORKSPACE, "workspace needs %zu bytes (256-byte aligned), got %zu", L.total,
               ws_bytes);

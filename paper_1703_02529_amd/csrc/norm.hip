@@ -624,6 +624,7 @@ struct NormPlan {
   int32_t parts;            // 1: one launch
 };
 
+constexpr int64_t kPartBytes = 16384;  // a part is at least that much
 constexpr int32_t kResident[] = {2, 4, 6, 8, 10, 12, 16, 20};
 
 // How a call is split, by its sizes and alignment alone.  max_count images.
@@ -654,7 +655,8 @@ NormPlan plan_norm(const nsc_norm_desc& d, uintptr_t ptrs, int64_t max_count, bo
     auto groups_for = [&](int64_t bytes) {  // at most 256 vectors wide, if it can be
       int32_t best = 0;
       for (int32_t g = 1; g <= d.groups; ++g) {
-        if (d.groups % g || (g * cpg) % p.ve || g * cpg / p.ve > (best ? 256 : most_t)) continue;
+        if (g * cpg / p.ve > (best ? 256 : most_t)) break;
+        if (d.groups % g || (g * cpg) % p.ve) continue;
         best = g;
         if ((int64_t)g * cpg * es >= bytes) break;
       }
@@ -709,7 +711,7 @@ NormPlan plan_norm(const nsc_norm_desc& d, uintptr_t ptrs, int64_t max_count, bo
   if (p.v == 0) p.threads = p.cv > 512 ? 1024 : 512;  // over 512: single elements
   if (items > 0 && p.v == 0 && items < 2 * kNumCU) {
     int64_t parts = (4 * kNumCU + items - 1) / items;
-    if (parts > bytes / 16384) parts = bytes / 16384;
+    if (parts > bytes / kPartBytes) parts = bytes / kPartBytes;
     if (parts > steps) parts = steps;
     if (parts > kMaxParts) parts = kMaxParts;
     if (parts > 1) {
@@ -817,15 +819,29 @@ int launch_norm_typed(int32_t dtype, const NormArgs& a, const NormPlan& p, bool 
   return launch_type<float>(a, p, backward, st);
 }
 
-// The parts' statistics: for any alignment, since it is known only at the call.
-size_t norm_ws_bytes(const nsc_norm_desc& d, int64_t max_count, bool backward) {
+// The parts' statistics of a call of count images: for any alignment of its
+// tensors (gradients: and for the sums over images).
+size_t norm_call_bytes(const nsc_norm_desc& d, int64_t count, bool backward) {
   int64_t parts = 1;
-  for (uintptr_t align = 16; align > 0; align /= 2) {
-    const NormPlan p = plan_norm(d, align, max_count, backward);
+  for (uintptr_t align = 16; align >= (uintptr_t)type_bytes(d.dtype); align /= 2) {
+    const NormPlan p = plan_norm(d, align, count, backward);
     if (p.parts > parts) parts = p.parts;
   }
-  if (backward) return (size_t)max_count * parts * d.c * 8;
-  return parts > 1 ? (size_t)max_count * parts * d.groups * 8 : 0;
+  if (backward) return (size_t)count * parts * d.c * 8;
+  return parts > 1 ? (size_t)count * parts * d.groups * 8 : 0;
+}
+
+// Of every call of up to max_count images.  Fewer images are split into more
+// parts, so that a smaller call can need more; from 2 kNumCU on, and where an
+// image does not make two parts, none is split.
+size_t norm_ws_bytes(const nsc_norm_desc& d, int64_t max_count, bool backward) {
+  size_t most = norm_call_bytes(d, max_count, backward);
+  if ((int64_t)d.h * d.w * d.c * type_bytes(d.dtype) < 2 * kPartBytes) return most;
+  for (int64_t n = 1; n < max_count && n < 2 * kNumCU; ++n) {
+    const size_t b = norm_call_bytes(d, n, backward);
+    if (b > most) most = b;
+  }
+  return most;
 }
 
 int check_call(const nsc_norm_desc* d, int64_t max_count, const void* ws, size_t ws_bytes,
@@ -833,7 +849,7 @@ int check_call(const nsc_norm_desc* d, int64_t max_count, const void* ws, size_t
   if (int rc = check_norm(d)) return rc;
   NSC_REQUIRE_L(max_count >= 0 && max_count <= kMaxImages, NSC_E_INVAL, "max_count %lld out of range",
                 (long long)max_count);
-  const size_t need = norm_ws_bytes(*d, max_count, backward);
+  const size_t need = norm_call_bytes(*d, max_count, backward);
   NSC_REQUIRE_L(need == 0 || (ws != nullptr && (uintptr_t)ws % 256 == 0 && ws_bytes >= need),
                 NSC_E_WORKSPACE, "workspace needs %zu bytes (256-byte aligned), got %zu", need,
                 ws_bytes);

@@ -306,6 +306,9 @@ struct SharedDense {
   size_t ws_bytes;
 };
 nsc_adapter_desc shared_desc(const Cnn& cnn, const nsc_group_adapters& ad);
+// Workspace of one nsc_adapter_project of that many rows (a call of fewer may
+// need more).
+size_t adapter_call_bytes(const nsc_adapter_desc& d, int64_t rows);
 
 struct CnnRunArgs {
   const int32_t* sums;

@@ -188,3 +188,37 @@ def test_the_gradients_take_fewer_rows_than_32_bits_count():
         assert _project_bwd(d, n=n, ws_bytes=1 << 60) == nsc.NSC_E_INVAL
         with pytest.raises(nsc.NscError):
             nsc.nsc_adapter_workspace_bytes(d, n, backward=True)
+
+
+COUNTS = (1, 2, 3, 5, 16, 17, 40, 64, 100, 255, 256, 300, 500, 511, 512, 900, 1100, 2047, 4096,
+          8000, 8192, 8193, 20000)
+
+
+@pytest.mark.parametrize("backward", [False, True])
+@pytest.mark.parametrize("kw", [
+    dict(h=112, w=112, c=320, groups=32), dict(h=200, w=300, c=8, groups=1),
+    dict(h=60, w=60, c=320, groups=320, dtype=nsc.NSC_T_F32), dict(h=100, w=100, c=17, groups=1),
+    dict(h=37, w=41, c=45, groups=5), dict(h=25, w=25, c=64, groups=8),
+    dict(h=40, w=40, c=700, groups=1), dict(h=1, w=1, c=16, groups=4),
+    dict(h=30, w=30, c=4096, groups=64), dict(h=9, w=9, c=16384, groups=16384)])
+def test_a_norm_workspace_holds_smaller_calls(kw, backward):
+    """The workspace "for up to max_count images" is enough for every smaller
+    call (a call without x is refused for that, once its workspace is checked)."""
+    d, call = _norm(**kw), (_norm_bwd if backward else _norm_fwd)
+    sizes = [nsc.nsc_group_norm_workspace_bytes(d, n, backward=backward) for n in COUNTS]
+    for i, n in enumerate(COUNTS):
+        for size in sizes[i:]:
+            assert call(d, x=None, n=n, ws_bytes=size) == nsc.NSC_E_INVAL, (n, size)
+
+
+@pytest.mark.parametrize("backward", [False, True])
+@pytest.mark.parametrize("kw", [
+    dict(), dict(k=4096, d=4096, rank=16), dict(k=9216, d=128, rank=16, dtype=nsc.NSC_T_F32),
+    dict(k=4608, d=32, rank=1, n_adapters=1, dtype=nsc.NSC_T_F32), dict(k=64, d=9216, rank=128),
+    dict(k=2 ** 20, d=1, rank=3), dict(k=1, d=1, rank=1), dict(k=2304, d=2304, rank=64)])
+def test_an_adapter_workspace_holds_smaller_calls(kw, backward):
+    d, call = _adapter(**kw), (_project_bwd if backward else _project)
+    sizes = [nsc.nsc_adapter_workspace_bytes(d, n, backward=backward) for n in COUNTS]
+    for i, n in enumerate(COUNTS):
+        for size in sizes[i:]:
+            assert call(d, x=None, n=n, ws_bytes=size) == nsc.NSC_E_INVAL, (n, size)
