@@ -76,12 +76,13 @@ __device__ __forceinline__ float act_floor(int act) {
   return act == NSC_ACT_RELU ? 0.0f : -__builtin_inff();
 }
 
-// (na, ma, qa) joined with (nb, mb, qb), nb > 0.
+// (na, ma, qa) joined with (nb, mb, qb), nb > 0.  (Joined with nothing, the
+// means' distance is not squared: it is the mean itself.)
 __device__ __forceinline__ void join(float& na, float& ma, float& qa, float nb, float mb,
                                      float qb) {
-  const float n = na + nb, f = nb / n, d = mb - ma;
+  const float n = na + nb, f = nb / n, d = mb - ma, dq = na > 0.0f ? d : 0.0f;
   ma += d * f;
-  qa += qb + d * d * na * f;
+  qa += qb + dq * dq * na * f;
   na = n;
 }
 
