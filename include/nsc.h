@@ -516,7 +516,7 @@ int nsc_group_norm(const nsc_norm_desc* desc, const void* x, const float* gamma,
  *   dx = rstd (gamma dz - m1 - xh m2), m1 and m2 the means of gamma dz and of
  *   gamma dz xh over the image's group.
  * dx as x; dgamma, dbeta (device, c floats) are written, zeros without
- * images.  The sums are taken in a fixed order.  Errors as above. */
+ * images.  The outputs must not overlap the inputs.  The sums are taken in a fixed order.  Errors as above. */
 int nsc_group_norm_backward(const nsc_norm_desc* desc, const void* x, const void* dy,
                             const float* gamma, const float* beta, const float* stats,
                             const int32_t* count, int64_t max_count, void* dx, float* dgamma,
@@ -546,7 +546,7 @@ int nsc_adapter_workspace_bytes(const nsc_adapter_desc* desc, int64_t max_rows, 
  * [n_adapters][rank][k]); b (device, [n_adapters][d][rank]); scale (device,
  * n_adapters floats); ids (device, int32 per row, in any order): a row whose
  * id lies outside 0 .. n_adapters - 1 (such as -1) has no adapter.  y must not
- * overlap the inputs.  Errors: NSC_E_INVAL, NSC_E_SHAPE, NSC_E_DTYPE,
+ * overlap the inputs (y == x is refused).  Errors: NSC_E_INVAL, NSC_E_SHAPE, NSC_E_DTYPE,
  * NSC_E_WORKSPACE, NSC_E_HIP. */
 int nsc_adapter_project(const nsc_adapter_desc* desc, const void* x, const void* w,
                         const float* bias, const void* a, const void* b, const float* scale,
@@ -558,7 +558,9 @@ int nsc_adapter_project(const nsc_adapter_desc* desc, const void* x, const void*
  *   dx[r] = dy[r] w + u a[p] (nullable: not computed),
  *   da[p] = sum u^T x[r], db[p] = sum dy[r]^T t over the rows of adapter p
  * (device, fp32, laid out as a and b; zeros for an adapter without rows).
- * The sums are taken in a fixed order.  Errors as above. */
+ * The outputs must not overlap the inputs: x and dy are read after dx is
+ * written (dx == x and dx == dy are refused).  The sums are taken in a fixed
+ * order.  Errors as above. */
 int nsc_adapter_backward(const nsc_adapter_desc* desc, const void* x, const void* dy,
                          const void* w, const void* a, const void* b, const float* scale,
                          const int32_t* ids, const int32_t* count, int64_t max_rows, void* dx,

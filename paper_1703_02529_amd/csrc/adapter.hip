@@ -1369,6 +1369,7 @@ int nsc_adapter_project(const nsc_adapter_desc* desc, const void* x, const void*
                     !misaligned(b, es) && !misaligned(y, es) && !misaligned(bias, 4) &&
                     !misaligned(scale, 4) && !misaligned(ids, 4) && !misaligned(count, 4),
                 NSC_E_INVAL, "a pointer is not aligned to its elements");
+  NSC_REQUIRE_L(y != x, NSC_E_INVAL, "y overlaps x");
   AdapterArgs g = adapter_args(*desc, w, a, b, scale, ids, count, max_rows);
   g.x = x;
   g.bias = bias;
@@ -1395,6 +1396,8 @@ int nsc_adapter_backward(const nsc_adapter_desc* desc, const void* x, const void
                     !misaligned(scale, 4) && !misaligned(ids, 4) && !misaligned(count, 4) &&
                     !misaligned(da, 4) && !misaligned(db, 4),
                 NSC_E_INVAL, "a pointer is not aligned to its elements");
+  NSC_REQUIRE_L(!dx || max_rows == 0 || (dx != x && dx != dy), NSC_E_INVAL,
+                "dx overlaps x or dy, which are read after it is written");
   const AdapterArgs g =
       adapter_args(*desc, w, a, b, scale, ids, max_rows ? count : nullptr, max_rows);
   unsigned char* at = static_cast<unsigned char*>(ws);

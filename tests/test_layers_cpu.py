@@ -222,3 +222,13 @@ def test_an_adapter_workspace_holds_smaller_calls(kw, backward):
     for i, n in enumerate(COUNTS):
         for size in sizes[i:]:
             assert call(d, x=None, n=n, ws_bytes=size) == nsc.NSC_E_INVAL, (n, size)
+
+
+def test_outputs_over_the_adapters_inputs_are_refused():
+    """x and dy are read after dx is written, and rows of x after rows of y."""
+    d, Q = _adapter(k=128, d=128), 1 << 20
+    assert _project(d, x=P, y=P, w=Q, a=Q, b=Q, scale=Q, ids=Q) == nsc.NSC_E_INVAL
+    assert "overlaps" in nsc.last_error()
+    for other in (dict(x=P, dy=Q), dict(x=Q, dy=P)):
+        assert _project_bwd(d, dx=P, w=Q, a=Q, b=Q, scale=Q, ids=Q, **other) == nsc.NSC_E_INVAL
+        assert "overlaps" in nsc.last_error()
