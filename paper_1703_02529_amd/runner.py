@@ -10,6 +10,7 @@ from __future__ import annotations
 
 from typing import Optional
 
+import numpy as np
 import torch
 
 from . import (NSC_METRIC_MSE, NSC_REF_FIXED, NSC_REF_PREV, Cnn, Group, SharedGroup, make_cfg,
@@ -109,8 +110,9 @@ class GroupRunner:
     frame geometry and metric), each with its weight blob and its device LR
     weights / reference sums (None where unused).  Runs n frames of every
     camera per call, camera-major.  With adapters = (rank, a, b, scale,
-    of_camera), as SharedGroup takes them, the cameras share the one network of
-    blobs[0]."""
+    of_camera), as SharedGroup takes them, the cameras share one network: the
+    descriptions' networks must be alike, and blobs holds the one blob (once, or
+    the same for every camera)."""
 
     def __init__(self, wls, blobs, frames_per_cam: int, lr_ws=None, ref_sums=None,
                  device="cuda", adapters=None):
@@ -120,6 +122,17 @@ class GroupRunner:
         self.lr_ws = list(lr_ws) if lr_ws is not None else [None] * k
         self.ref_sums = list(ref_sums) if ref_sums is not None else [None] * k
         self.cfgs = [_cfg_of(w, l, r) for w, l, r in zip(self.wls, self.lr_ws, self.ref_sums)]
+        blobs = list(blobs)
+        if adapters is not None:
+            nets = {(tuple(n.conv), tuple(n.pool), n.dense, n.in_h, n.in_w, bool(n.bf16))
+                    for n in (w.cnn for w in self.wls)}
+            if len(nets) > 1:
+                raise ValueError("cameras with adapters share one network: theirs differ")
+            if len(blobs) not in (1, k) or any(b is not blobs[0] and
+                                               not np.array_equal(b, blobs[0]) for b in blobs):
+                raise ValueError("cameras with adapters share one network: one blob, or the same "
+                                 "for every camera, expected")
+            blobs = blobs[:1]
         self.cnns = [Cnn(make_desc(w.cnn.conv, w.cnn.pool, w.cnn.dense, w.cnn.in_h, w.cnn.in_w,
                                    w.cnn.bf16), b) for w, b in zip(self.wls, blobs)]
         if adapters is None:

@@ -232,3 +232,38 @@ def test_outputs_over_the_adapters_inputs_are_refused():
     for other in (dict(x=P, dy=Q), dict(x=Q, dy=P)):
         assert _project_bwd(d, dx=P, w=Q, a=Q, b=Q, scale=Q, ids=Q, **other) == nsc.NSC_E_INVAL
         assert "overlaps" in nsc.last_error()
+
+
+def test_cameras_with_adapters_have_one_network(monkeypatch):
+    """A runner of a shared network packs it once, and refuses networks or weights
+    that differ from camera to camera."""
+    np = pytest.importorskip("numpy")
+    import dataclasses
+
+    from paper_1703_02529_amd import runner
+    from synth import workloads as W
+
+    class Made(Exception):
+        pass
+
+    made = []
+
+    def shared(cfgs, cnn, *adapters):
+        raise Made(len(cfgs), cnn, adapters)
+
+    monkeypatch.setattr(runner, "Cnn", lambda desc, blob: made.append(blob) or len(made))
+    monkeypatch.setattr(runner, "SharedGroup", shared)
+    ads, blob = (4, "a", "b", "scale", "of"), np.arange(5, dtype=np.float32)
+    wls = [W.TINY.replace(c_low=0.2 + 0.1 * c) for c in range(3)]
+    for blobs in ([blob], [blob] * 3, [blob, blob.copy(), blob.copy()]):
+        made.clear()
+        with pytest.raises(Made) as e:
+            runner.GroupRunner(wls, blobs, 10, adapters=ads)
+        assert e.value.args == (3, 1, ads) and len(made) == 1 and made[0] is blob
+    made.clear()
+    other = wls[2].replace(cnn=dataclasses.replace(W.TINY.cnn, dense=64))
+    for bad, blobs in ((wls, [blob, blob, blob + 1]), (wls, [blob, blob]), (wls, []),
+                       (wls[:2] + [other], [blob])):
+        with pytest.raises(ValueError, match="share one network"):
+            runner.GroupRunner(bad, blobs, 10, adapters=ads)
+    assert not made
