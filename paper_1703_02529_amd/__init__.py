@@ -411,8 +411,8 @@ class Group:
 class SharedGroup(Group):
     """A group whose cameras share one fp32 network and differ by adapters of its
     dense layer: a [n_adapters][rank][features], b [n_adapters][dense][rank],
-    scale [n_adapters] (device, fp32) and of_camera (device, int32 per camera).
-    They must outlive the group, which keeps them."""
+    scale [n_adapters] (fp32) and of_camera (int32 per camera), on the current
+    device.  They must outlive the group, which keeps them."""
 
     def __init__(self, cfgs, cnn, rank, a, b, scale, of_camera):
         import torch
@@ -427,6 +427,10 @@ class SharedGroup(Group):
         _hold("b", b, torch.float32, n * rank * desc.dense)
         _hold("scale", scale, torch.float32, n)
         _hold("of_camera", of_camera, torch.int32, n_cams)
+        for t in (a, b, scale, of_camera):  # the group's tables and network are there
+            if t.is_cuda and t.get_device() != torch.cuda.current_device():
+                raise ValueError(f"tensors on the current device {torch.cuda.current_device()} "
+                                 f"expected, got one on device {t.get_device()}")
         self.n_cams = n_cams
         self._cfgs = (CascadeCfg * n_cams)(*cfgs)
         self.cnns = [cnn]

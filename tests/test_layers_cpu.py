@@ -267,3 +267,38 @@ def test_cameras_with_adapters_have_one_network(monkeypatch):
         with pytest.raises(ValueError, match="share one network"):
             runner.GroupRunner(bad, blobs, 10, adapters=ads)
     assert not made
+
+
+class _Elsewhere:
+    """What the binding asks of a tensor, on a device of the test's choice."""
+
+    def __init__(self, dtype, numel, device):
+        self.dtype, self._n, self._d, self.is_cuda = dtype, numel, device, True
+
+    def numel(self):
+        return self._n
+
+    def get_device(self):
+        return self._d
+
+    def is_contiguous(self):
+        return True
+
+    def data_ptr(self):
+        return P
+
+
+def test_a_shared_group_takes_adapters_of_the_current_device(monkeypatch):
+    torch = pytest.importorskip("torch")
+    import types
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    cnn = types.SimpleNamespace(desc=nsc.make_desc([16], [0], 16, 8, 8, False), handle=None)
+    cfg = nsc.make_cfg(in_h=16, in_w=16, dd_h=8, dd_w=8, cnn_h=8, cnn_w=8)
+    need = dict(a=(torch.float32, 2 * 3 * 16 * 64), b=(torch.float32, 2 * 3 * 16),
+                scale=(torch.float32, 2), of_camera=(torch.int32, 1))
+    for away in (None, *need):
+        at = [_Elsewhere(t, n, int(k == away)) for k, (t, n) in need.items()]
+        # on the current device: on to the library, which refuses the missing network
+        with pytest.raises(ValueError if away else nsc.NscError,
+                           match="device 1" if away else "network handle"):
+            nsc.SharedGroup([cfg], cnn, 3, *at)
