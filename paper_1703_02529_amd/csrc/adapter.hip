@@ -11,6 +11,7 @@
 //
 // The gradients of the adapters are sums over an adapter's rows, which a list
 // of the rows by adapter gives in ascending order.
+#include "adapter_plan.h"
 #include "layer_types.h"
 
 #include <limits.h>
@@ -290,8 +291,6 @@ __device__ __forceinline__ void adapter_down(const AdapterArgs& a, int64_t block
 
 // The rank-wide rows alone in a launch: of one reduction (t of x and a), or of
 // two (and u of dy and the transposed b).
-constexpr int kDownWaves = 8, kGemmDownWaves = 4;
-constexpr int kMaxParts = 4, kMaxJoinParts = 8;  // of their reduction; beside a split product
 
 struct DownArgs {
   AdapterArgs of[2];
@@ -406,16 +405,16 @@ __device__ __forceinline__ void add_ranks(const AdapterArgs& a, f32x4 (&acc)[NI]
       tv[j] = f32x4{0.f, 0.f, 0.f, 0.f};
       todo[j] = with_adapter(mine[j]);
       if (mine[j] != INT_MAX) {
-        f32x4 v[kMaxParts];
+        f32x4 v[kMaxDownParts];
 #pragma unroll
-        for (int h = 0; h < kMaxParts; ++h) {
+        for (int h = 0; h < kMaxDownParts; ++h) {
           v[h] = f32x4{0.f, 0.f, 0.f, 0.f};
           if (h == 0 || h < a.t_parts)
             v[h] = *reinterpret_cast<const f32x4*>(
                 a.t + (h * a.max_rows + pos0 + j * 16 + m) * a.rp + q);
         }
 #pragma unroll
-        for (int h = 0; h < kMaxParts; ++h) tv[j] += v[h];
+        for (int h = 0; h < kMaxDownParts; ++h) tv[j] += v[h];
       }
     }
     auto load_b = [&](int p, f32x4 (&bv)[NI]) __attribute__((always_inline)) {
@@ -938,12 +937,12 @@ __global__ void __launch_bounds__(512) k_adapter_grad(GradArgs a) {
           const float* ts = t + (int64_t)(r + 4 * g + s) * a.rp + j0 + m;
           uv[s] = in ? *ts : 0.0f;
           if constexpr (!decltype(one)::value) {
-            float part[kMaxParts - 1];
+            float part[kMaxDownParts - 1];
 #pragma unroll
-            for (int h = 1; h < kMaxParts; ++h)
+            for (int h = 1; h < kMaxDownParts; ++h)
               part[h - 1] = in && h < parts ? ts[h * a.max_rows * a.rp] : 0.0f;
 #pragma unroll
-            for (int h = 1; h < kMaxParts; ++h) uv[s] += part[h - 1];
+            for (int h = 1; h < kMaxDownParts; ++h) uv[s] += part[h - 1];
           }
         }
         next_rows(r + 16 * RW);
@@ -1014,111 +1013,6 @@ int check_adapter(const nsc_adapter_desc* d) {
   return NSC_OK;
 }
 
-// How a product is split: tiles of tn outputs x tm rows and parts of the
-// reduction, chosen by the sizes alone.
-struct GemmPlan {
-  int32_t tn, tm, parts;
-};
-
-GemmPlan plan_gemm(int64_t max_rows, int64_t outs, int64_t len, int64_t es, bool tr) {
-  GemmPlan p{};
-  // Large tiles read each operand least often; they need enough of them to
-  // fill the chip
-  auto tiles = [&](int64_t tn, int64_t tm) {
-    return (outs + tn - 1) / tn * ((max_rows + tm - 1) / tm);
-  };
-  const int64_t blocks = (len * es + 127) / 128;
-  const bool few = !tr && outs <= 64 && max_rows > 16;
-  const bool big = !few && tiles(256, 128) >= kNumCU && blocks >= 16;
-  p.tn = big ? 256 : 128;
-  p.tm = big ? 128 : max_rows <= 16 ? 16 : 64;
-  // Up to 64 outputs would leave half of a tile of 128 to multiply zeros, which
-  // counts where the matrix instructions are slow: 3,038 rows of 4,608 values
-  // onto 32 outputs in fp32 took 91 us with 128 and take 61 with 64.  Backward
-  // the tiles run over the inputs, which are many.
-  if (few) p.tn = 64;
-  const int64_t t = tiles(p.tn, p.tm);
-  // parts for about a workgroup per CU, each of at least four blocks
-  int64_t parts = t > 0 ? kNumCU / t : 1;
-  if (parts > blocks / 4) parts = blocks / 4;
-  if (parts > 64) parts = 64;
-  p.parts = parts < 1 ? 1 : (int32_t)parts;
-  return p;
-}
-
-size_t gemm_part_bytes(const GemmPlan& p, int64_t max_rows, int64_t outs) {
-  if (p.parts == 1) return 0;
-  return (size_t)((outs + p.tn - 1) / p.tn * p.tn) * ((max_rows + p.tm - 1) / p.tm * p.tm) *
-         p.parts * 4;
-}
-
-// Parts of the rank-wide rows' reduction: about two workgroups per CU, four of
-// the smaller ones beside a split product, each wave of at least two chunks of
-// 128 bytes.
-int32_t down_parts(int64_t max_rows, int64_t len, int64_t es, bool split) {
-  const int64_t tiles = (max_rows + 15) / 16, per = split ? 4 : 2;
-  int64_t parts = tiles > 0 ? per * kNumCU / tiles : 1;
-  const int64_t most = len * es / (128 * 2 * (split ? kGemmDownWaves : kDownWaves));
-  if (parts > most) parts = most;
-  if (parts > (split ? kMaxJoinParts : kMaxParts)) parts = split ? kMaxJoinParts : kMaxParts;
-  return parts < 1 ? 1 : (int32_t)parts;
-}
-
-// From this many rows on they are taken in the order of their adapters, so that
-// 16 neighbours mostly share one.
-constexpr int64_t kListRows = 256;
-
-// Workspace: the rank-wide rows t (backward: and u) by part, the product's
-// partial sums, the rows by adapter, and backward b transposed.
-struct AdapterLayout {
-  size_t t, u, part, off, rows, bt, total;
-  int32_t t_parts, u_parts;
-  GemmPlan g;
-  bool list;
-};
-
-AdapterLayout adapter_layout(const nsc_adapter_desc& d, int64_t max_rows, bool backward) {
-  AdapterLayout L{};
-  size_t o = 0;
-  auto take = [&](size_t bytes) {
-    const size_t at = o;
-    o = align_up(o + bytes, 256);
-    return at;
-  };
-  const int64_t es = type_bytes(d.dtype);
-  const size_t rp = align_up(d.rank, 16);
-  L.g = backward ? plan_gemm(max_rows, d.k, d.d, es, true)
-                 : plan_gemm(max_rows, d.d, d.k, es, false);
-  L.t_parts = down_parts(max_rows, d.k, es, !backward && L.g.parts > 1);
-  L.u_parts = down_parts(max_rows, d.d, es, false);
-  L.list = backward || max_rows >= kListRows;
-  L.t = take((size_t)max_rows * rp * 4 * L.t_parts);
-  if (backward) {
-    L.u = take((size_t)max_rows * rp * 4 * L.u_parts);
-    if (max_rows > 0) L.bt = take((size_t)d.n_adapters * d.rank * d.d * es);
-  }
-  L.part = take(gemm_part_bytes(L.g, max_rows, backward ? d.k : d.d));
-  if (L.list) {
-    L.off = take(((size_t)d.n_adapters + 1) * 4);
-    L.rows = take((size_t)max_rows * 4);
-  }
-  L.total = o;
-  return L;
-}
-
-// Of every call of up to max_rows rows.  Fewer rows are split into more parts,
-// so that a smaller call can need more.  Between multiples of 16 rows a call
-// only grows, and from 8,192 rows on neither reduction is split: 128 tiles of 64
-// rows leave a tile fewer than two parts, 512 tiles of 16 its rank-wide rows.
-size_t adapter_ws_bytes(const nsc_adapter_desc& d, int64_t max_rows, bool backward) {
-  size_t most = adapter_layout(d, max_rows, backward).total;
-  for (int64_t n = 16; n < max_rows && n <= 8192; n += 16) {
-    const size_t b = adapter_layout(d, n, backward).total;
-    if (b > most) most = b;
-  }
-  return most;
-}
-
 int check_adapter_call(const nsc_adapter_desc* d, int64_t max_rows, const void* ws,
                        size_t ws_bytes, bool backward) {
   if (int rc = check_adapter(d)) return rc;
@@ -1180,14 +1074,10 @@ int launch_gemm(const AdapterArgs& a, const GemmPlan& p, bool vec, hipStream_t s
   return vec ? launch_plan<T, true, TR>(a, p, st) : launch_plan<T, false, TR>(a, p, st);
 }
 
-// Waves share an adapter's rows where its columns alone make too few of them
-// (about two per SIMD) and it has two steps of 16 rows for each on average.
 template <typename T>
 int launch_grad(GradArgs a, int32_t n_adapters, int64_t max_rows, hipStream_t st) {
   constexpr int CPL = 16 / sizeof(T);
-  const int64_t waves = ((int64_t)a.cols[0] + a.cols[1]) / (16 * CPL) * n_adapters;
-  int rw = 1;
-  while (rw < 8 && waves * rw < 8 * kNumCU && max_rows / n_adapters >= 2 * 16 * 2 * rw) rw *= 2;
+  const int rw = grad_row_waves((int64_t)a.cols[0] + a.cols[1], n_adapters, max_rows, sizeof(T));
   const int32_t width = 16 * CPL * (8 / rw);
   a.blocks0 = (a.cols[0] + width - 1) / width;
   const dim3 g((unsigned)(a.blocks0 + (a.cols[1] + width - 1) / width), (unsigned)n_adapters),

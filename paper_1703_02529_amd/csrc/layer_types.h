@@ -12,8 +12,6 @@ namespace nsc {
     if (!(cond)) return ::nsc::fail(code, __VA_ARGS__); \
   } while (0)
 
-inline int64_t type_bytes(int32_t dtype) { return dtype == NSC_T_F32 ? 4 : 2; }
-
 // VE consecutive elements as one load or store.
 template <typename T, int VE>
 struct alignas(sizeof(T) * VE) Vec {

@@ -5,6 +5,7 @@
 #include <stdint.h>
 
 #include "nsc.h"
+#include "sizes.h"
 
 namespace nsc {
 
@@ -25,9 +26,6 @@ int fail(int code, const char* fmt, ...) __attribute__((format(printf, 2, 3)));
       return ::nsc::fail(NSC_E_HIP, "launch of %s failed: %s", what, hipGetErrorString(e_)); \
   } while (0)
 
-constexpr int kNumCU = 256;  // MI355X compute units (8 XCDs x 32)
-constexpr int kNumXCD = 8;
-
 // Logical index of workgroup b of a grid of nb: the hardware hands workgroup b
 // to XCD b mod 8, so numbering each XCD's workgroups consecutively gives each
 // XCD one contiguous range of the logical work (in its dispatch order), whose
@@ -37,17 +35,6 @@ __device__ __forceinline__ int64_t xcd_block(int64_t b, int64_t nb) {
   const int64_t q = nb / kNumXCD, r = nb % kNumXCD;
   return x * q + (x < r ? x : r) + slot;
 }
-
-inline int64_t gcd64(int64_t a, int64_t b) {
-  while (b) {
-    int64_t t = a % b;
-    a = b;
-    b = t;
-  }
-  return a;
-}
-
-inline size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 
 // Exact area resampling of one axis: output cell o covers [o*p, (o+1)*p) and
 // input pixel i covers [i*q, (i+1)*q), both in units of 1/q input pixel.
