@@ -511,12 +511,13 @@ int nsc_group_norm(const nsc_norm_desc* desc, const void* x, const float* gamma,
                    size_t ws_bytes, void* stream);
 /* The gradients of the above for the gradient dy of its output, from the same
  * x and the stats it wrote.  With xh = (x - mean) * rstd, z = gamma xh + beta
- * and dz = dy * act'(z) (ReLU: dy where z > 0, decided exactly):
+ * and dz = dy * act'(z) (ReLU: dy where z > 0, decided in fp64):
  *   dbeta[ch] = sum dz, dgamma[ch] = sum dz xh over all images and pixels,
  *   dx = rstd (gamma dz - m1 - xh m2), m1 and m2 the means of gamma dz and of
  *   gamma dz xh over the image's group.
  * dx as x; dgamma, dbeta (device, c floats) are written, zeros without
- * images.  The outputs must not overlap the inputs.  The sums are taken in a fixed order.  Errors as above. */
+ * images.  The outputs must not overlap the inputs.  The sums are taken in a
+ * fixed order.  Errors as above. */
 int nsc_group_norm_backward(const nsc_norm_desc* desc, const void* x, const void* dy,
                             const float* gamma, const float* beta, const float* stats,
                             const int32_t* count, int64_t max_count, void* dx, float* dgamma,

@@ -57,7 +57,8 @@ inline int32_t down_parts(int64_t max_rows, int64_t len, int64_t es, bool split)
   int64_t parts = tiles > 0 ? per * kNumCU / tiles : 1;
   const int64_t most = len * es / (128 * 2 * (split ? kGemmDownWaves : kDownWaves));
   if (parts > most) parts = most;
-  if (parts > (split ? kMaxJoinParts : kMaxDownParts)) parts = split ? kMaxJoinParts : kMaxDownParts;
+  const int64_t room = split ? kMaxJoinParts : kMaxDownParts;
+  if (parts > room) parts = room;
   return parts < 1 ? 1 : (int32_t)parts;
 }
 

@@ -61,7 +61,11 @@ __device__ __forceinline__ int64_t live_count(const NormArgs& a) {
 }
 
 // The activation of VE values; `floor` is what the values are cut at below (0
-// for ReLU, minus infinity without an activation).  NaN stays.
+// for ReLU, minus infinity without an activation).  NaN stays.  SiLU's
+// exponential and reciprocal are the instructions of the machine, for fp32 too:
+// their error, |z| and a few roundings of 2^-24, is that of z itself (128 maps of
+// 50x50x64 fp32: mean error 0.89 (gradient) and 1.01 of that of the elementary
+// operations in fp32).
 template <int VE>
 __device__ __forceinline__ void activate(float (&z)[VE], int act, float floor) {
   if (act == NSC_ACT_SILU) {
@@ -425,8 +429,8 @@ __global__ void __launch_bounds__(VE == 1 ? 1024 : 512) k_norm_grad(NormArgs a) 
         }
     };
     // xh and dz = dy act'(z) of vector u, z = (x - mean) gamma rstd + beta.  The
-    // ReLU's sign is that of the exact value: fp32's z is within 2^-22 of its
-    // product of it, and values closer to zero are taken again in fp64.
+    // ReLU's sign is fp64's: fp32's z is within 2^-22 of its product of the exact
+    // one, and values closer to zero are taken again in fp64.
     auto grads = [&](int u, float (&dz)[VE], float (&xh)[VE]) __attribute__((always_inline)) {
       xv[u].renew();
       gv[u].renew();
@@ -456,6 +460,9 @@ __global__ void __launch_bounds__(VE == 1 ? 1024 : 512) k_norm_grad(NormArgs a) 
       for (int e = 0; e < VE; ++e) xh[e] = (f[e] - mu[K > 1 ? e : 0]) * rs[K > 1 ? e : 0];
     };
     if constexpr (P != NormPass::Apply) {
+      // (fp32 over an image's pixels, fp64 over images: of the sums of 128 maps of
+      // 50x50x64 fp32 the mean error is 1.2 to 2.3 x 2^-24 of their mean size, that
+      // of sums all in fp64 0.4 to 1.3)
       float s1[VE], s2[VE];
 #pragma unroll
       for (int e = 0; e < VE; ++e) s1[e] = s2[e] = 0.0f;
@@ -716,8 +723,8 @@ int launch_norm_typed(int32_t dtype, const NormArgs& a, const NormPlan& p, bool 
 int check_call(const nsc_norm_desc* d, int64_t max_count, const void* ws, size_t ws_bytes,
                bool backward) {
   if (int rc = check_norm(d)) return rc;
-  NSC_REQUIRE_L(max_count >= 0 && max_count <= kMaxImages, NSC_E_INVAL, "max_count %lld out of range",
-                (long long)max_count);
+  NSC_REQUIRE_L(max_count >= 0 && max_count <= kMaxImages, NSC_E_INVAL,
+                "max_count %lld out of range", (long long)max_count);
   const size_t need = norm_call_bytes(*d, max_count, backward);
   NSC_REQUIRE_L(need == 0 || (ws != nullptr && (uintptr_t)ws % 256 == 0 && ws_bytes >= need),
                 NSC_E_WORKSPACE, "workspace needs %zu bytes (256-byte aligned), got %zu", need,
