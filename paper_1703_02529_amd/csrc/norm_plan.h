@@ -124,7 +124,7 @@ inline NormPlan plan_norm(const nsc_norm_desc& d, uintptr_t ptrs, int64_t max_co
   p.parts = 1;
   const int64_t items = max_count * p.blocks, bytes = hw * p.cb * es;
   if (p.threads == 1024 && items < 2 * kNumCU && bytes > 32768) p.v = 0;
-  if (p.v == 0) p.threads = p.cv > 512 ? 1024 : 512;  // over 512: single elements
+  if (p.v == 0) p.threads = p.cv > 512 ? 1024 : 512;  // (backward, 1,024: single elements)
   if (items > 0 && p.v == 0 && items < 2 * kNumCU) {
     int64_t parts = (4 * kNumCU + items - 1) / items;
     if (parts > bytes / kPartBytes) parts = bytes / kPartBytes;
